@@ -397,7 +397,7 @@ def _plain_accept(s, c):
             p = torch.where(refused[b, x], 0.0, p)
             take = tried & (u[:, n] * mass < p)
             drop = tried & ~take
-            mass = torch.where(drop, mass - p, mass)
+            mass = torch.where(drop, (mass - p).clamp(min=0.0), mass)
             refused[b, x] |= drop & inside
         depth = depth + take
         cur = torch.where(take, n, cur)
@@ -552,7 +552,7 @@ def _exact_accept(s, c):
                     if u[b, child] * gone < px:
                         down = int(child)
                         break
-                    gone -= px
+                    gone = max(gone - px, 0.0)
                     if 0 <= x < V:
                         now[x] = 0.0
             if down is None:

@@ -315,6 +315,127 @@ int sv_commit_path(const sv_model_cfg *cfg, const sv_kv_view *kv, int T, const i
 int sv_advance_prefix(int32_t *prefix_len, const int32_t *accepted_len, int B, int d_cap,
                       void *stream);
 
+/* ---- Sampled acceptance: probabilities from logits, walk down the tree by random numbers ---- */
+
+#define SV_MAX_SAMPLED_VOCAB (1 << 22) /* columns of a row of probabilities */
+
+/* probs[i][j] = exp(logits[i][j] / temperature) / sum over the row: what the heads' out_logits
+ * become before sv_sampled_accept.  logits, probs: [device] float32 [n_rows, n_vocab]; probs may be
+ * logits.  Maximum and sum are float32.  A row of nothing but -infinity (everything masked) becomes
+ * zeros; a row that holds a NaN or +infinity becomes NaN.
+ * SV_ERR_SHAPE unless 1 <= n_rows < 2^31 / 1024, 1 <= n_vocab <= SV_MAX_SAMPLED_VOCAB; SV_ERR_TOKEN unless
+ * temperature is a number above zero, finite like its reciprocal (for the greedy choice there is sv_relaxed_accept). */
+int sv_token_probs(const float *logits, int n_rows, int n_vocab, float temperature, float *probs,
+                   void *stream);
+
+/* Acceptance that keeps the target's distribution, next to sv_relaxed_accept (Alg. 1 with the
+ * acceptance test of speculative sampling in the place of Eq. 5): walks down each of B trees from
+ * the root.  At node n, p = target_prob[n] (the verifier's distribution behind n) and the children
+ * of n are tried in ascending order against u = u_accept[child]:
+ *   draft_prob given: q = draft_prob[n], from which the drafter drew every child of n (independently;
+ *     equal children are fine).  With less = 0, mass = 1 at first, child x is accepted when
+ *     u q(x) mass < max(p(x) - less q(x), 0); a refusal adds mass to less, and mass becomes the sum
+ *     of max(p - less q, 0).  (The closed form of replacing p by norm(max(p - q, 0)) each time.)
+ *   draft_prob NULL: the children are the drafter's own choice, such as its most probable tokens
+ *     (sv_tree_build_device).  With mass = 1 at first, child x is accepted when u mass < p(x), p(x) of a
+ *     token that was refused before counting as 0; a refusal takes p(x) off mass (down to 0).
+ * An accepted child becomes n.  Where no child is accepted, where there is none, or at depth d_cap, the walk
+ * ends, and the token behind it is drawn from what is left, max(p - less q, 0) or p without the
+ * refused tokens: the first one whose cumulated sum exceeds u_draw * total (the last one with any
+ * mass if none does).  Emitted tokens are then distributed as the target's, whatever the drafter did.
+ * All arithmetic is float64 on the float32 inputs, in a fixed order: the results are reproducible.
+ *   tree: as for sv_relaxed_accept; only tree->parent and n_nodes = T are read (a parent that is not
+ *     an earlier node makes its node nobody's child)
+ *   draft_token:  [device] int32[B*T] (entry 0 of each tree unused)
+ *   target_prob, draft_prob: [device] float32 [B*T, n_vocab], columns = token ids vocab_lo ..
+ *     vocab_lo + n_vocab - 1, rows taken as normalised (sv_token_probs); draft_prob may be NULL.
+ *     Rows of nodes that the walk does not reach are not read.  A token outside the columns has p = q = 0:
+ *     it is never accepted.  A NaN counts as no mass.
+ *   u_accept: [device] float32[B*T], u_draw: [device] float32[B]: uniform numbers in [0, 1)
+ *   accept_mask, accepted_len, best_node, path, out_tokens: [device, out] as sv_relaxed_accept
+ *     leaves them (accept_mask is 1 on the path only), so that sv_commit_path and sv_advance_prefix
+ *     follow as they do there; out_tokens ends with the drawn token
+ *   status: [device, out] int32[B]: 0 = ok; bit 0 = nothing was left to draw from and the draw was
+ *     made from p; bit 1 = p has no mass either, the token is vocab_lo
+ * SV_ERR_SHAPE for B < 1, B > 2^15, bad T or d_cap (see sv_relaxed_accept) or n_vocab outside
+ * 1 .. SV_MAX_SAMPLED_VOCAB; SV_ERR_TOKEN if vocab_lo < 0 or vocab_lo + n_vocab exceeds 2^31 - 1. */
+int sv_sampled_accept(const sv_tree *tree, const int32_t *draft_token, const float *target_prob,
+                      const float *draft_prob, int n_vocab, int vocab_lo, const float *u_accept,
+                      const float *u_draw, int B, int d_cap, uint8_t *accept_mask,
+                      int32_t *accepted_len, int32_t *best_node, int32_t *path,
+                      int32_t *out_tokens, int32_t *status, void *stream);
+
+/* ---- Paged key-value cache: append, attention of one new token per sequence ------------------
+ *
+ * For decoding token by token next to the tree pass - the draft model's steps, the verifier where
+ * nothing is drafted - with sequences of any length in one pool.  Rows 0 .. len-1 of sequence s are
+ * its keys and values; row j lies in page block_table[s][j / page_size] at row j % page_size.
+ * One layer's cache of the verifier (sv_kv_view, [B][n_heads][capacity][head_dim]) is a paged one
+ * too where its capacity is a multiple of 16: n_pages = n_seqs = B, page_size = capacity,
+ * max_pages = 1, block_table[s][0] = s. */
+#define SV_MAX_PAGED_HEAD_DIM 256
+typedef struct sv_paged_cache {
+  void *k, *v;                /* [device] [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
+  const int32_t *block_table; /* [device] int32 [n_seqs][max_pages]; entries behind a sequence's last page are not read */
+  int32_t dtype;              /* SV_F32 or SV_BF16 (the cache of 8-bit and 4-bit weight models too) */
+  int32_t n_seqs, max_pages, n_pages;
+  int32_t page_size;          /* a multiple of 16 */
+  int32_t n_kv_heads;
+  int32_t head_dim;           /* a multiple of 8, at most SV_MAX_PAGED_HEAD_DIM */
+} sv_paged_cache;
+
+/* Rotates new keys (RoPE, rotate-half pairs i and i + head_dim/2, angle pos * theta^(-2i/head_dim) in
+ * float64) and writes them with their values to the cache; rotates the tokens' queries.
+ *   token_seq, token_pos: [device] int32[n_tokens]: sequence and row of each token, in any order;
+ *     no two of one call the same.  token_seq < 0 marks a padding row of the batch: nothing of it is
+ *     read or written.
+ *   q, k, v: [device] float32, token t at q + t * q_stride ([n_q_heads][head_dim] inside), k + t *
+ *     k_stride, v + t * v_stride ([n_kv_heads][head_dim]): parts of a fused projection fit; 16-byte
+ *     aligned, strides (in elements) multiples of 4.  q may be NULL (n_q_heads = 0 then): keys and values only.
+ *   q_out: [device, out] float32 [n_tokens, n_q_heads, head_dim] contiguous, or NULL with q; may be
+ *     q itself where q_stride = n_q_heads * head_dim
+ *   status: [device, out] int32[n_tokens] or NULL: 0 = written, 1 = padding, 2 = token_seq or
+ *     token_pos outside the block table, 4 = its page outside the pool; only tokens of status 0 are
+ *     written (their queries too)
+ * Lengths are the caller's: a row counts once the next call's seq_len covers it, and lowering seq_len
+ * takes drafted tokens back.  Layout sizes are checked as for sv_paged_attention.
+ * SV_ERR_SHAPE for n_tokens outside 1 .. 2^22, strides below a token's own elements, alignments, or
+ * theta not above zero. */
+int sv_paged_append(const sv_paged_cache *cache, int n_tokens, const int32_t *token_seq,
+                    const int32_t *token_pos, const float *q, int n_q_heads, long long q_stride,
+                    const float *k, long long k_stride, const float *v, long long v_stride,
+                    float rope_theta, float *q_out, int32_t *status, void *stream);
+
+/* Host-only.  Bytes of device scratch that sv_paged_attention needs for lengths up to max_len ->
+ * *bytes; never less than for a smaller max_len, and enough for every window.  The scratch needs no
+ * preparation, and a call leaves nothing in it for the next: calls that share one must not overlap. */
+int sv_paged_workspace_bytes(const sv_paged_cache *cache, int n_q_heads, int max_len, size_t *bytes);
+
+/* Attention of the newest token of every sequence (row seq_len[s] - 1, appended before) over its
+ * visible rows: all of them, or with window > 0 the last `window` rows (the new token among them)
+ * and the first n_sink rows of the sequence.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   out[s][h] = sum_j w_j V_j,  w = softmax over visible j of scale * q[s][h] . K_j
+ *   seq_len: [device] int32[n_seqs], clamped to 0 .. max_len; max_len: [host value] upper bound, used
+ *     for planning; at most max_pages * page_size
+ *   q: [device] float32 [n_seqs, n_q_heads, head_dim] (rotated), 16-byte aligned
+ *   out: [device, out] float32, laid out as q; may be q.  lse: [device, out] float32 [n_seqs, n_q_heads]
+ *     or NULL: log of the sum of exp(scale * q . K_j), with which results over parts of a cache are joined
+ *   status: [device, out] int32[n_seqs] or NULL: 1 = the page of a visible row is outside 0 ..
+ *     n_pages - 1 (such rows count as not visible), 0 otherwise
+ *   workspace: [device], 256-byte aligned, ws_bytes >= sv_paged_workspace_bytes
+ * A sequence without visible rows (length 0) gets zeros and lse = -infinity.  Rows that are not visible may
+ * hold anything, NaN and infinity too.  A NaN or infinity in a visible row or a query makes at most
+ * the outputs of the heads that read it NaN or infinite; which of the two is not specified.
+ * Scores, softmax and outputs are float32; with a bf16 cache queries and weights enter the matrix
+ * cores as sums of three bf16 numbers (2^-24 of each value).  Results are the same in every run.
+ * SV_ERR_DTYPE for other cache types; SV_ERR_SHAPE if a size or alignment is outside the rules
+ * above, n_q_heads is no multiple of n_kv_heads, n_seqs or n_q_heads exceeds 2^15, max_pages *
+ * page_size 2^30, or scale is not finite; SV_ERR_WORKSPACE if the scratch is too small or misaligned. */
+int sv_paged_attention(const sv_paged_cache *cache, const int32_t *seq_len, int max_len,
+                       const float *q, int n_q_heads, float scale, int window, int n_sink,
+                       float *out, float *lse, int32_t *status, void *workspace, size_t ws_bytes,
+                       void *stream);
+
 #ifdef __cplusplus
 }
 #endif

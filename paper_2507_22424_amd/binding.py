@@ -20,6 +20,8 @@ SV_F32, SV_BF16, SV_BF16_W8, SV_BF16_W4 = 0, 1, 2, 3
  SV_ERR_LAUNCH) = (0, -1, -2, -3, -4, -5, -6, -7)
 SV_MAX_TREE_NODES = 128
 SV_MAX_DEPTH = 31
+SV_MAX_SAMPLED_VOCAB = 1 << 22
+SV_MAX_PAGED_HEAD_DIM = 256
 SV_WS_ATTN_OUT, SV_WS_Q, SV_WS_STATUS = 0, 1, 2
 
 EXPORTS = ("sv_version", "sv_strerror", "sv_tree_build_masks", "sv_packed_layer_bytes",
@@ -28,7 +30,9 @@ EXPORTS = ("sv_version", "sv_strerror", "sv_tree_build_masks", "sv_packed_layer_
            "sv_verify_layer_timed", "sv_verify_stack", "sv_product_plan",
            "sv_action_head_argmax", "sv_action_head_argmax_noalloc", "sv_packed_head_bytes", "sv_pack_head",
            "sv_action_head_argmax_packed", "sv_stream_read", "sv_relaxed_accept",
-           "sv_commit_path", "sv_advance_prefix", "sv_tree_build_device")
+           "sv_commit_path", "sv_advance_prefix", "sv_tree_build_device",
+           "sv_token_probs", "sv_sampled_accept", "sv_paged_append", "sv_paged_workspace_bytes",
+           "sv_paged_attention")
 SV_N_TIMING_EVENTS = 9
 SV_PLAN_QKV, SV_PLAN_OUT, SV_PLAN_GATE_UP, SV_PLAN_DOWN, SV_PLAN_HEAD = range(5)
 SV_KERNEL_SKINNY, SV_KERNEL_MID, SV_KERNEL_THIN = range(3)
@@ -62,6 +66,12 @@ class KvView(C.Structure):
 class Tree(C.Structure):
     _fields_ = [("parent", C.c_void_p), ("depth", C.c_void_p), ("anc_mask", C.c_void_p),
                 ("n_nodes", C.c_int32), ("n_words", C.c_int32)]
+
+
+class PagedView(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("block_table", C.c_void_p), ("dtype", C.c_int32),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
 _lib = None
@@ -121,6 +131,17 @@ def lib() -> C.CDLL:
         l.sv_tree_build_device.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
                                            C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        l.sv_token_probs.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p]
+        l.sv_sampled_accept.argtypes = [C.POINTER(Tree), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
+                                        C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        l.sv_paged_append.argtypes = [C.POINTER(PagedView), C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                      C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p, C.c_longlong, C.c_float,
+                                      C.c_void_p, C.c_void_p, C.c_void_p]
+        l.sv_paged_workspace_bytes.argtypes = [C.POINTER(PagedView), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+        l.sv_paged_attention.argtypes = [C.POINTER(PagedView), C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_float,
+                                         C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_size_t, C.c_void_p]
         _lib = l
     return _lib
 
@@ -423,6 +444,99 @@ def sv_tree_build_device(cand_parent: torch.Tensor, cand_logp: torch.Tensor, can
         _dev(status, torch.int32, "status"), _stream(stream)), "sv_tree_build_device")
 
 
+def _one_device(**tensors) -> None:
+    """The tensors of a call lie on the device that it is launched on, the current one."""
+    current = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for name, t in tensors.items():
+        if t is not None and t.device.index != current:
+            raise ValueError(f"{name} is on {t.device}, the current device is {current}")
+
+
+def sv_token_probs(logits: torch.Tensor, temperature: float, probs: torch.Tensor, stream=None) -> None:
+    """probs = softmax(logits / temperature) of [rows, vocabulary]; `probs` may be `logits`."""
+    if logits.dim() != 2 or probs.shape != logits.shape:
+        raise ValueError("token_probs: logits and probs must be [rows, vocabulary]")
+    args = (_dev(logits, torch.float32, "logits"), logits.shape[0], logits.shape[1], temperature,
+            _dev(probs, torch.float32, "probs"))
+    _one_device(logits=logits, probs=probs)
+    _check(lib().sv_token_probs(*args, _stream(stream)), "sv_token_probs")
+
+
+def sv_sampled_accept(tree: Tree, draft_token: torch.Tensor, target_prob: torch.Tensor,
+                      draft_prob: Optional[torch.Tensor], vocab_lo: int, u_accept: torch.Tensor,
+                      u_draw: torch.Tensor, B: int, d_cap: int, accept_mask: torch.Tensor,
+                      accepted_len: torch.Tensor, best_node: torch.Tensor, path: torch.Tensor,
+                      out_tokens: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    T = tree.n_nodes
+    n_vocab = target_prob.shape[-1]
+    if target_prob.numel() != B * T * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
+            draft_token.numel() != B * T or u_accept.numel() != B * T or u_draw.numel() != B or \
+            accept_mask.numel() != B * T or accepted_len.numel() != B or best_node.numel() != B or \
+            status.numel() != B or path.numel() != B * (d_cap + 1) or out_tokens.numel() != B * (d_cap + 1):
+        raise ValueError("sampled_accept: tensor sizes do not match B, T, d_cap")
+    args = (_dev(draft_token, torch.int32, "draft_token"), _dev(target_prob, torch.float32, "target_prob"),
+            _dev(draft_prob, torch.float32, "draft_prob"), n_vocab, vocab_lo, _dev(u_accept, torch.float32, "u_accept"),
+            _dev(u_draw, torch.float32, "u_draw"), B, d_cap, _dev(accept_mask, torch.uint8, "accept_mask"),
+            _dev(accepted_len, torch.int32, "accepted_len"), _dev(best_node, torch.int32, "best_node"),
+            _dev(path, torch.int32, "path"), _dev(out_tokens, torch.int32, "out_tokens"), _dev(status, torch.int32, "status"))
+    _one_device(target_prob=target_prob, draft_prob=draft_prob, draft_token=draft_token, u_accept=u_accept, u_draw=u_draw,
+                accept_mask=accept_mask, accepted_len=accepted_len, best_node=best_node, path=path,
+                out_tokens=out_tokens, status=status)
+    _check(lib().sv_sampled_accept(C.byref(tree), *args, _stream(stream)), "sv_sampled_accept")
+
+
+def _token_rows(t: Optional[torch.Tensor], n_tokens: int, heads: Optional[int], d: int, name: str) -> Tuple[int, int, int]:
+    """(pointer, heads, stride in elements) of [tokens, heads, d] whose tokens may lie apart."""
+    if t is None:
+        return 0, 0, 0
+    if not t.is_cuda or t.dtype != torch.float32:
+        raise ValueError(f"{name} must be a float32 device tensor")
+    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != d or (heads is not None and t.shape[1] != heads) or \
+            t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must be [{n_tokens}, {heads or 'heads'}, {d}] with contiguous tokens")
+    return t.data_ptr(), t.shape[1], t.stride(0) if n_tokens > 1 else t.shape[1] * d
+
+
+def sv_paged_append(cache: "PagedCache", token_seq: torch.Tensor, token_pos: torch.Tensor, q: Optional[torch.Tensor],
+                    k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor], rope_theta: float,
+                    status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, k, v: [tokens, heads, head_dim] float32, views of a fused projection among them."""
+    n, c = token_seq.numel(), cache.struct
+    if token_pos.numel() != n or (status is not None and status.numel() != n) or (q is None) != (q_out is None) or \
+            (q is not None and q_out.shape != q.shape):
+        raise ValueError("paged_append: tensor sizes do not match the tokens")
+    qp, n_q, q_stride = _token_rows(q, n, None, c.head_dim, "q")
+    kp, _, k_stride = _token_rows(k, n, c.n_kv_heads, c.head_dim, "k")
+    vp, _, v_stride = _token_rows(v, n, c.n_kv_heads, c.head_dim, "v")
+    args = (n, _dev(token_seq, torch.int32, "token_seq"), _dev(token_pos, torch.int32, "token_pos"), qp, n_q, q_stride,
+            kp, k_stride, vp, v_stride, rope_theta, _dev(q_out, torch.float32, "q_out"), _dev(status, torch.int32, "status"))
+    _one_device(cache=cache.k, token_seq=token_seq, token_pos=token_pos, q=q, k=k, v=v, q_out=q_out, status=status)
+    _check(lib().sv_paged_append(C.byref(c), *args, _stream(stream)), "sv_paged_append")
+
+
+def sv_paged_workspace_bytes(cache: "PagedCache", n_q_heads: int, max_len: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().sv_paged_workspace_bytes(C.byref(cache.struct), n_q_heads, max_len, C.byref(out)),
+           "sv_paged_workspace_bytes")
+    return out.value
+
+
+def sv_paged_attention(cache: "PagedCache", seq_len: torch.Tensor, max_len: int, q: torch.Tensor, scale: float,
+                       window: int, n_sink: int, out: torch.Tensor, lse: Optional[torch.Tensor],
+                       status: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """q, out: [sequences, query heads, head_dim] float32; window 0: every row is visible."""
+    c = cache.struct
+    if q.dim() != 3 or q.shape[0] != c.n_seqs or q.shape[2] != c.head_dim or out.shape != q.shape or \
+            seq_len.numel() != c.n_seqs or (lse is not None and lse.numel() != c.n_seqs * q.shape[1]) or \
+            (status is not None and status.numel() != c.n_seqs):
+        raise ValueError("paged_attention: tensor sizes do not match the cache")
+    args = (_dev(seq_len, torch.int32, "seq_len"), max_len, _dev(q, torch.float32, "q"), q.shape[1], scale, window, n_sink,
+            _dev(out, torch.float32, "out"), _dev(lse, torch.float32, "lse"), _dev(status, torch.int32, "status"),
+            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    _one_device(cache=cache.k, seq_len=seq_len, q=q, out=out, lse=lse, status=status, workspace=workspace)
+    _check(lib().sv_paged_attention(C.byref(c), *args, _stream(stream)), "sv_paged_attention")
+
+
 # ---- holders that keep the device tensors behind the C structs alive -------------------
 
 class DeviceTree:
@@ -454,3 +568,26 @@ class KvCache:
                            else torch.from_numpy(pl).to(device))
         self.struct = KvView(self.k.data_ptr(), self.v.data_ptr(), self.prefix_len.data_ptr(),
                              int(pl.max()), capacity)
+
+
+class PagedCache:
+    """Pool of key and value pages of one layer, [n_pages, n_kv_heads, page_size, head_dim] each, and the block
+    table of its sequences, int32 [n_seqs, max_pages]; the table's entries may be rewritten between calls."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or block_table.dim() != 2:
+            raise ValueError("k and v must be [n_pages, n_kv_heads, page_size, head_dim], block_table [n_seqs, max_pages]")
+        if k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"a paged cache holds float32 or bfloat16, got {k.dtype}")
+        if k.device != v.device or k.device != block_table.device:
+            raise ValueError("pages and block table must lie on one device")
+        self.k, self.v, self.block_table = k, v, block_table
+        self.struct = PagedView(_dev(k, name="k"), _dev(v, name="v"), _dev(block_table, torch.int32, "block_table"),
+                                SV_F32 if k.dtype == torch.float32 else SV_BF16, block_table.shape[0],
+                                block_table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3])
+
+    @classmethod
+    def of_kv_cache(cls, kv: "KvCache") -> "PagedCache":
+        """One layer's contiguous cache (capacity a multiple of 16) as pages: episode b is page b."""
+        B = kv.k.shape[0]
+        return cls(kv.k, kv.v, torch.arange(B, dtype=torch.int32, device=kv.k.device)[:, None].contiguous())

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libspecvla_verify.so")
 SOURCES = [os.path.join(HERE, "csrc", n + ".hip")
-           for n in ["sv_api", "sv_plan"] + [f"sv_{family}_{epi}" for family in ("mid", "skinny")
+           for n in ["sv_api", "sv_plan", "sv_sample", "sv_paged"] + [f"sv_{family}_{epi}" for family in ("mid", "skinny")
                                              for epi in ("swiglu", "qkv", "resid", "out")]]
 OBJ_DIR = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

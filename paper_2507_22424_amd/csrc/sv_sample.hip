@@ -1,0 +1,54 @@
+// C-ABI entry points of the sampled acceptance: argument checks and launches.
+#include <cmath>
+
+#include "sv_sample.h"
+
+namespace sv {
+
+static int token_probs(const float* logits, int n_rows, int n_vocab, float temperature, float* probs, hipStream_t st) {
+  if (!logits || !probs) return SV_ERR_NULL;
+  if (n_rows < 1 || n_rows >= (1 << 21) || n_vocab < 1 || n_vocab > SV_MAX_SAMPLED_VOCAB) return SV_ERR_SHAPE;
+  const float inv_t = 1.f / temperature;
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t)) return SV_ERR_TOKEN;
+  if (n_vocab > 2048) token_probs_kernel<1024><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
+  else token_probs_kernel<64><<<n_rows, 64, 0, st>>>(logits, n_vocab, inv_t, probs);
+  return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH;
+}
+
+static int sampled_accept(const SampleArgs& a, int B, hipStream_t st) {
+  if (a.n_vocab > 2048) sampled_accept_kernel<1024><<<B, 1024, 0, st>>>(a);
+  else sampled_accept_kernel<256><<<B, 256, 0, st>>>(a);
+  return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH;
+}
+
+}  // namespace sv
+
+using namespace sv;
+
+extern "C" {
+
+int sv_token_probs(const float* logits, int n_rows, int n_vocab, float temperature, float* probs, void* stream) {
+  return token_probs(logits, n_rows, n_vocab, temperature, probs, (hipStream_t)stream);
+}
+
+int sv_sampled_accept(const sv_tree* tree, const int32_t* draft_token, const float* target_prob, const float* draft_prob,
+                      int n_vocab, int vocab_lo, const float* u_accept, const float* u_draw, int B, int d_cap,
+                      uint8_t* accept_mask, int32_t* accepted_len, int32_t* best_node, int32_t* path, int32_t* out_tokens,
+                      int32_t* status, void* stream) {
+  if (!tree || !tree->parent || !draft_token || !target_prob || !u_accept || !u_draw || !accept_mask || !accepted_len ||
+      !best_node || !path || !out_tokens || !status)
+    return SV_ERR_NULL;
+  const int T = tree->n_nodes;
+  if (B < 1 || B > (1 << 15) || T < 1 || T > SV_MAX_TREE_NODES || d_cap < 0 || d_cap > SV_MAX_DEPTH || n_vocab < 1 ||
+      n_vocab > SV_MAX_SAMPLED_VOCAB)
+    return SV_ERR_SHAPE;
+  if (vocab_lo < 0 || (long long)vocab_lo + n_vocab > 0x7fffffffll) return SV_ERR_TOKEN;
+  SampleArgs a;
+  a.parent = tree->parent; a.token = draft_token; a.target = target_prob; a.draft = draft_prob;
+  a.u_accept = u_accept; a.u_draw = u_draw; a.T = T; a.n_vocab = n_vocab; a.lo = vocab_lo; a.d_cap = d_cap;
+  a.accept_mask = accept_mask; a.accepted_len = accepted_len; a.best_node = best_node; a.path = path;
+  a.out_tokens = out_tokens; a.status = status;
+  return sampled_accept(a, B, (hipStream_t)stream);
+}
+
+}  // extern "C"

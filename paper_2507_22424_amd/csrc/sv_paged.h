@@ -75,77 +75,378 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
 }
 
 // ---- attention ---------------------------------------------------------------------------------
+// Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T, on matrix instructions whose 16 columns are
+// the query heads of one KV head.  A lane holds one query column c = lane % 16 and, of a unit of 16 keys,
+// the scores of keys 4g .. 4g+3 (g = lane / 16), which are the weights that the second product wants of it: nothing
+// moves between lanes.  K rows are operands as they lie in the page (lane: key c, a slice of the head); of V
+// a lane takes the rows of its own four keys, 16 bytes each, and a register of the V^T operand is two halves of
+// registers that it holds already.  LDS is used once, to join the waves.
+// Units are 16 rows of a page at a multiple of 16, so that a unit lies in one page and its address is scalar.
 
 struct PagedAttnArgs {
   PagedCache c;
   const int32_t* seq_len;
   int max_len, n_q, window, n_sink;
-  float scale;
+  int n_blocks;              // blocks of 16 query heads per KV head
+  int n_split, split_units;  // workgroups that share a sequence's units, units of each (a multiple of 2)
+  float scale;               // with log2(e)
   const float* q;
   float *out, *lse;
   int32_t* status;
+  float *part, *part_ml;     // [rows][n_split][d], [rows][n_split][2]
 };
 
-// grid = (query heads, sequences), block = 256: four waves take the visible rows in turn, a lane holds up to four
-// columns; running maximum and sum per wave, joined through LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attention_rows(const PagedAttnArgs a) {
-  __shared__ float s_m[4], s_l[4], s_o[4][SV_MAX_PAGED_HEAD_DIM];
-  __shared__ int s_bad;
-  const int h = blockIdx.x, s = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, d = a.c.d;
-  const int hk = h / (a.n_q / a.c.n_kv);
-  int len = a.seq_len[s];
-  len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
-  int n_sink = 0, first = 0;                 // visible: 0 .. n_sink - 1 and first .. len - 1
-  if (a.window > 0 && len > a.window) {
-    first = len - a.window;
-    n_sink = min(a.n_sink, first);
-  }
-  const int n_seen = n_sink + len - first;
-  const size_t qrow = ((size_t)s * a.n_q + h) * d;
-  if (threadIdx.x == 0) s_bad = 0;
-  __syncthreads();
-  float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) q[e] = e * 64 + lane < d ? a.q[qrow + e * 64 + lane] * a.scale : 0.f;
-  for (int i = wave; i < n_seen; i += 4) {
-    const int j = i < n_sink ? i : first + (i - n_sink);
-    const int page = a.c.table[(size_t)s * a.c.max_pages + j / a.c.page_size];
-    if (page < 0 || page >= a.c.n_pages) {
-      if (lane == 0) s_bad = 1;
-      continue;
+// Units of 16 rows that hold a visible row: those of the first rows, then those of the window.
+struct VisibleRows {
+  int len, first, n_sink;    // visible: 0 .. n_sink - 1 and first .. len - 1
+  int sink_units, main_unit, n_units;
+  __host__ __device__ VisibleRows(int length, int max_len, int window, int sinks) {
+    len = length < 0 ? 0 : (length > max_len ? max_len : length);
+    first = n_sink = 0;
+    if (window > 0 && len > window) {
+      first = len - window;
+      n_sink = sinks < first ? sinks : first;
     }
-    const size_t at = (((size_t)page * a.c.n_kv + hk) * a.c.page_size + j % a.c.page_size) * d;
-    float x = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e * 64 + lane < d) x += q[e] * to_f32(((const T*)a.c.k)[at + e * 64 + lane]);
-    x = wave_sum(x);
-    const float m2 = fmaxf(m, x), f = m2 == -INFINITY ? 1.f : expf(m - m2), w = m2 == -INFINITY ? 0.f : expf(x - m2);
-    m = m2;
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e * 64 + lane < d) o[e] = o[e] * f + w * to_f32(((const T*)a.c.v)[at + e * 64 + lane]);
+    sink_units = (n_sink + 15) / 16;
+    main_unit = first / 16 > sink_units ? first / 16 : sink_units;
+    const int end = (len + 15) / 16;
+    n_units = sink_units + (end > main_unit ? end - main_unit : 0);
   }
-  if (lane == 0) {
-    s_m[wave] = m;
-    s_l[wave] = l;
+  __device__ int unit(int u) const { return u < sink_units ? u : u - sink_units + main_unit; }
+  __device__ bool full(int unit) const {
+    return unit * 16 + 16 <= len && (unit * 16 >= first || unit * 16 + 16 <= n_sink);
   }
+  __device__ bool sees(int j) const { return j < len && (j >= first || j < n_sink); }
+};
+
+__device__ inline f32x4_t mfma_bf16(uint4 a, uint4 b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// x = hi + mid + lo, bf16 each (24 bits: x itself, but for what lies below 2^-24 of it)
+__device__ inline void split8_3(const float* v, uint4* part) {
+  float r[8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) s_o[wave][e * 64 + lane] = o[e];
+  for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pack_bf16x2(r[2 * e], r[2 * e + 1]);
+      r[2 * e] -= bf16_lo_f32(w[e]);
+      r[2 * e + 1] -= bf16_hi_f32(w[e]);
+    }
+    part[p] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// A tile of the cache in registers and its two products.  DP: head_dim rounded up to 64, 128 or 256 (columns
+// behind head_dim: q is zero, K and V repeat columns of the row, and the outputs are not stored).
+template <typename T, int DP>
+struct PagedTile;
+
+template <int DP>
+struct PagedTile<bf16_t, DP> {
+  static constexpr int kUnits = 2, kSteps = DP / 32, kOut = DP / 16;
+  static constexpr int kE = DP / 16 < 8 ? DP / 16 : 8, kLoads = DP / 16 / kE;    // V: elements of a load, loads of a row
+  static constexpr int kScores = 8;
+  uint4 k[2][kSteps];
+  uint32_t v[8][kE / 2 * kLoads];
+  uint4 q[kSteps][3];
+
+  static __device__ int out_col(int t, int m) { return t / kE * 16 * kE + kE * m + t % kE; }
+  __device__ void load_q(const float* src, bool real, float scale, int d, int g) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = real && 32 * s + 8 * g < d ? src[32 * s + 8 * g + e] * scale : 0.f;
+      split8_3(x, q[s]);
+    }
+  }
+  __device__ void load_k(int u, const char* base, int d, int g, int c) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int col = min(32 * s + 8 * g, d - 8);
+      k[u][s] = *(const uint4*)(base + (unsigned)(c * d + col) * 2u);
+    }
+  }
+  __device__ void load_v(int u, const char* base, int d, int g, int c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int l = 0; l < kLoads; ++l) {
+        const char* p = base + (unsigned)((4 * g + r) * d + min(128 * l + kE * c, d - kE)) * 2u;
+        uint32_t* dst = v[4 * u + r] + l * (kE / 2);
+        if constexpr (kE == 8) {
+          const uint4 w = *(const uint4*)p;
+          dst[0] = w.x; dst[1] = w.y; dst[2] = w.z; dst[3] = w.w;
+        } else {
+          const uint2 w = *(const uint2*)p;
+          dst[0] = w.x; dst[1] = w.y;
+        }
+      }
+  }
+  __device__ void drop_v(int e) {
+#pragma unroll
+    for (int w = 0; w < kE / 2 * kLoads; ++w) v[e][w] = 0;
+  }
+  __device__ void scores(float* x) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) s = mfma_bf16(k[u][i], q[i][2 - p], s);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[4 * u + r] = s[r];
+    }
+  }
+  __device__ void add(const float* p, f32x4_t* o) const {
+    uint4 w[3];
+    split8_3(p, w);
+#pragma unroll
+    for (int t = 0; t < kOut; ++t) {
+      const unsigned sel = t & 1 ? 0x07060302u : 0x05040100u;
+      uint4 a;
+      a.x = __builtin_amdgcn_perm(v[1][t / 2], v[0][t / 2], sel);
+      a.y = __builtin_amdgcn_perm(v[3][t / 2], v[2][t / 2], sel);
+      a.z = __builtin_amdgcn_perm(v[5][t / 2], v[4][t / 2], sel);
+      a.w = __builtin_amdgcn_perm(v[7][t / 2], v[6][t / 2], sel);
+#pragma unroll
+      for (int i = 2; i >= 0; --i) o[t] = mfma_bf16(a, w[i], o[t]);
+    }
+  }
+};
+
+template <int DP>
+struct PagedTile<float, DP> {
+  static constexpr int kUnits = 1, kSteps = DP / 16, kOut = DP / 16;
+  static constexpr int kScores = 4;
+  f32x4_t k[1][kSteps], v[4][DP / 64], q[kSteps];
+
+  static __device__ int out_col(int t, int m) { return t / 4 * 64 + 4 * m + t % 4; }
+  __device__ void load_q(const float* src, bool real, float scale, int d, int g) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[s][e] = real && 16 * s + 4 * g < d ? src[16 * s + 4 * g + e] * scale : 0.f;
+  }
+  __device__ void load_k(int, const char* base, int d, int g, int c) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k[0][s] = *(const f32x4_t*)(base + (unsigned)(c * d + min(16 * s + 4 * g, d - 4)) * 4u);
+  }
+  __device__ void load_v(int, const char* base, int d, int g, int c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int l = 0; l < DP / 64; ++l)
+        v[r][l] = *(const f32x4_t*)(base + (unsigned)((4 * g + r) * d + min(64 * l + 4 * c, d - 4)) * 4u);
+  }
+  __device__ void drop_v(int e) {
+#pragma unroll
+    for (int l = 0; l < DP / 64; ++l) v[e][l] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ void scores(float* x) const {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[i][e], s, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = s[r];
+  }
+  __device__ void add(const float* p, f32x4_t* o) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < kOut; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][t / 4][t % 4], p[r], o[t], 0, 0, 0);
+  }
+};
+
+// One workgroup = (sequence, KV head, block of 16 query heads, split); its four waves take tiles in turn.
+// grid.x = sequences * KV heads * splits * blocks.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(const PagedAttnArgs a) {
+  using Tile = PagedTile<T, DP>;
+  constexpr int kU = Tile::kUnits, kPitch = DP + 4;
+  __shared__ float s_m[4][16], s_l[4][16];
+  __shared__ __attribute__((aligned(16))) float s_o[4][16][kPitch];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int g = lane >> 4, c = lane & 15, d = a.c.d;
+  unsigned id = blockIdx.x;
+  const int hb = id % a.n_blocks;
+  id /= a.n_blocks;
+  const int split = id % a.n_split;
+  id /= a.n_split;
+  const int hk = id % a.c.n_kv, seq = id / a.c.n_kv;
+  const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
+  const int u_begin = split * a.split_units, u_end = min(rows.n_units, u_begin + a.split_units);
+  if (u_begin >= u_end && split > 0) return;
+  const int G = a.n_q / a.c.n_kv, n_heads = min(16, G - 16 * hb);
+  const size_t row0 = (size_t)seq * a.n_q + hk * G + 16 * hb;
+
+  Tile tile;
+  tile.load_q(a.q + (row0 + c) * d, c < n_heads, a.scale, d, g);
+  f32x4_t o[Tile::kOut];
+#pragma unroll
+  for (int t = 0; t < Tile::kOut; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  bool bad = false;
+
+  const int32_t* table = a.c.table + (size_t)seq * a.c.max_pages;
+  const int page_units = a.c.page_size / 16;
+  // where unit u of this sequence lies: offset in bytes, -1 where its page is none
+  auto locate = [&](int u) -> long long {
+    if (u >= u_end) return -1;
+    const int at = rows.unit(u), p = at / page_units;
+    const int page = __builtin_amdgcn_readfirstlane(table[p]);
+    if ((unsigned)page >= (unsigned)a.c.n_pages) {
+      bad = true;
+      return -1;
+    }
+    return (((long long)page * a.c.n_kv + hk) * a.c.page_size + (at - p * page_units) * 16) * d * (long long)sizeof(T);
+  };
+  long long at[kU], next[kU];
+  auto load_k = [&](const long long* w) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) tile.load_k(u, (const char*)a.c.k + (w[u] < 0 ? 0 : w[u]), d, g, c);
+  };
+  auto load_v = [&](const long long* w) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) tile.load_v(u, (const char*)a.c.v + (w[u] < 0 ? 0 : w[u]), d, g, c);
+  };
+  int u0 = u_begin + wave * kU;
+  if (u0 < u_end) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) at[u] = locate(u0 + u);
+    load_k(at);
+    load_v(at);
+  }
+  for (; u0 < u_end; u0 += 4 * kU) {
+    float x[Tile::kScores];
+    tile.scores(x);
+    const bool more = u0 + 4 * kU < u_end;
+    if (more) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) next[u] = locate(u0 + 4 * kU + u);
+      load_k(next);
+    }
+    bool full = true;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) full = full && at[u] >= 0 && rows.full(rows.unit(u0 + u));
+    if (!full) {
+#pragma unroll
+      for (int e = 0; e < Tile::kScores; ++e)
+        if (at[e / 4] < 0 || !rows.sees(rows.unit(u0 + e / 4) * 16 + 4 * g + e % 4)) {
+          x[e] = -INFINITY;
+          tile.drop_v(e);
+        }
+    }
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < Tile::kScores; ++e) top = fmaxf(top, x[e]);
+    // the maximum of a query moves in the first tiles and rarely afterwards
+    if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float m2 = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < Tile::kOut; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[t][r] *= f;
+    }
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float p[Tile::kScores];
+#pragma unroll
+    for (int e = 0; e < Tile::kScores; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(x[e] - m_use);
+      l += p[e];
+    }
+    tile.add(p, o);
+    if (more) load_v(next);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) at[u] = next[u];
+  }
+
+  // ---- join the waves ----
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  if (g == 0) {
+    s_m[wave][c] = m;
+    s_l[wave][c] = l;
+  }
+  if (c < n_heads) {
+#pragma unroll
+    for (int t = 0; t < Tile::kOut; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s_o[wave][c][Tile::out_col(t, 4 * g + r)] = o[t][r];
+  }
   __syncthreads();
-  float m_all = -INFINITY, l_all = 0.f, v = 0.f;
-  for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, s_m[w]);
-  for (int w = 0; w < 4; ++w) {
-    const float f = s_m[w] == -INFINITY ? 0.f : expf(s_m[w] - m_all);
-    l_all += f * s_l[w];
-    v += f * s_o[w][threadIdx.x];
+  for (int i = threadIdx.x; i < n_heads * (d / 4); i += 256) {
+    const int h = i / (d / 4), e = (i - h * (d / 4)) * 4;
+    float m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, s_m[w][h]);
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = s_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][h] - m_all);
+      l_all += f * s_l[w][h];
+      v += f * *(const f32x4_t*)&s_o[w][h][e];
+    }
+    const size_t row = row0 + h;
+    if (a.n_split > 1) {
+      *(f32x4_t*)(a.part + (row * a.n_split + split) * d + e) = v;
+      if (e == 0) {
+        a.part_ml[(row * a.n_split + split) * 2] = m_all;
+        a.part_ml[(row * a.n_split + split) * 2 + 1] = l_all;
+      }
+    } else {
+      if (l_all != 0.f) v *= 1.f / l_all;
+      *(f32x4_t*)(a.out + row * d + e) = v;
+      if (e == 0 && a.lse) a.lse[row] = l_all == 0.f ? -INFINITY : (m_all + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
+    }
   }
-  if ((int)threadIdx.x < d) a.out[qrow + threadIdx.x] = l_all > 0.f ? v / l_all : (l_all == 0.f ? 0.f : l_all);
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[(size_t)s * a.n_q + h] = l_all == 0.f ? -INFINITY : m_all + logf(l_all);
-    if (a.status && h == 0) a.status[s] = s_bad;
+  if (a.status && hk == 0 && hb == 0) {
+    // (one wave sees a bad page at least where there is one)
+    if (a.n_split == 1) {
+      const int any = __syncthreads_or(bad);
+      if (threadIdx.x == 0) a.status[seq] = any;
+    }
+  }
+}
+
+// Joins the splits of a row in their order; one wave looks over the pages of a sequence for the status.
+// grid = (query heads, sequences), block = 256.
+__global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs a) {
+  const int h = blockIdx.x, seq = blockIdx.y, d = a.c.d;
+  const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
+  const int n = max(1, (rows.n_units + a.split_units - 1) / a.split_units);
+  const size_t row = (size_t)seq * a.n_q + h;
+  const float* ml = a.part_ml + row * a.n_split * 2;
+  const float* part = a.part + row * a.n_split * d;
+  float m = -INFINITY, l = 0.f, v = 0.f;
+  for (int s = 0; s < n; ++s) m = fmaxf(m, ml[2 * s]);
+  for (int s = 0; s < n; ++s) {
+    const float f = ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2 * s] - m);
+    l += f * ml[2 * s + 1];
+    if ((int)threadIdx.x < d) v += f * part[(size_t)s * d + threadIdx.x];
+  }
+  if ((int)threadIdx.x < d) a.out[row * d + threadIdx.x] = l != 0.f ? v / l : 0.f;
+  if (threadIdx.x == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  if (a.status && h == 0) {
+    bool bad = false;
+    for (int u = threadIdx.x; u < rows.n_units; u += 256) {
+      const int page = a.c.table[(size_t)seq * a.c.max_pages + rows.unit(u) / (a.c.page_size / 16)];
+      bad |= (unsigned)page >= (unsigned)a.c.n_pages;
+    }
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) a.status[seq] = any;
   }
 }
 

@@ -25,6 +25,36 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   return SV_OK;
 }
 
+// How a call is split over the chip: kTargetGroups workgroups where the cache is long enough for that, each at
+// least kMinUnits units of 16 rows.  Splits (and with them the scratch) never get fewer as max_len grows.
+constexpr int kTargetGroups = 1024, kMinUnits = 16;
+struct PagedPlan {
+  int n_blocks, n_split, split_units;
+  size_t rows, part, part_ml, bytes;
+};
+static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
+  PagedPlan p;
+  p.n_blocks = ceil_div(n_q / c.n_kv_heads, 16);
+  const long long tasks = (long long)c.n_seqs * c.n_kv_heads * p.n_blocks;
+  const int most = (int)(tasks >= kTargetGroups ? 1 : (kTargetGroups + tasks - 1) / tasks);
+  const int fill = n_units / kMinUnits;
+  p.n_split = fill < 1 ? 1 : (fill < most ? fill : most);
+  p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
+  p.rows = (size_t)c.n_seqs * n_q;
+  p.part = 0;
+  p.part_ml = p.n_split > 1 ? align_up(p.rows * p.n_split * c.head_dim * 4, kAlign) : 0;
+  p.bytes = p.n_split > 1 ? p.part_ml + align_up(p.rows * p.n_split * 8, kAlign) : kAlign;
+  return p;
+}
+
+// Units that the visible rows of any sequence of up to max_len rows lie in, at most.
+static int most_units(int max_len, int window, int n_sink) {
+  const int all = ceil_div(max_len, 16);
+  if (window == 0) return all;
+  const long long some = (n_sink + 15ll) / 16 + (window + 15ll) / 16 + 1;      // (a window may begin inside a unit)
+  return some < all ? (int)some : all;
+}
+
 static int launch_status() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
 
 }  // namespace sv
@@ -60,7 +90,7 @@ int sv_paged_workspace_bytes(const sv_paged_cache* cache, int n_q_heads, int max
   int rc = check_paged(cache);
   if (rc == SV_OK) rc = check_heads(*cache, n_q_heads, max_len);
   if (rc != SV_OK) return rc;
-  *bytes = kAlign;
+  *bytes = plan_paged(*cache, n_q_heads, ceil_div(max_len, 16)).bytes;
   return SV_OK;
 }
 
@@ -73,12 +103,23 @@ int sv_paged_attention(const sv_paged_cache* cache, const int32_t* seq_len, int 
   if (!seq_len || !q || !out || !workspace) return SV_ERR_NULL;
   if (window < 0 || n_sink < 0 || !std::isfinite(scale) || (uintptr_t)q % 16 || (uintptr_t)out % 16) return SV_ERR_SHAPE;
   if ((uintptr_t)workspace % kAlign || ws_bytes < need) return SV_ERR_WORKSPACE;
+  const PagedPlan p = plan_paged(*cache, n_q_heads, most_units(max_len, window, n_sink));
   PagedAttnArgs a;
   a.c = view(*cache); a.seq_len = seq_len; a.max_len = max_len; a.n_q = n_q_heads; a.window = window; a.n_sink = n_sink;
-  a.scale = scale; a.q = q; a.out = out; a.lse = lse; a.status = status;
-  const dim3 grid(n_q_heads, cache->n_seqs);
-  if (cache->dtype == SV_F32) paged_attention_rows<float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-  else paged_attention_rows<bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+  a.n_blocks = p.n_blocks; a.n_split = p.n_split; a.split_units = p.split_units;
+  a.scale = scale * 1.4426950408889634f; a.q = q; a.out = out; a.lse = lse; a.status = status;
+  a.part = (float*)((char*)workspace + p.part); a.part_ml = (float*)((char*)workspace + p.part_ml);
+  hipStream_t st = (hipStream_t)stream;
+  const unsigned groups = (unsigned)((size_t)cache->n_seqs * cache->n_kv_heads * p.n_blocks * p.n_split);
+  auto run = [&](auto t) {
+    using T = decltype(t);
+    if (cache->head_dim <= 64) paged_attention_mfma<T, 64><<<groups, 256, 0, st>>>(a);
+    else if (cache->head_dim <= 128) paged_attention_mfma<T, 128><<<groups, 256, 0, st>>>(a);
+    else paged_attention_mfma<T, 256><<<groups, 256, 0, st>>>(a);
+  };
+  if (cache->dtype == SV_F32) run(0.f);
+  else run(bf16_t{});
+  if (p.n_split > 1) paged_attention_join<<<dim3(n_q_heads, cache->n_seqs), 256, 0, st>>>(a);
   return launch_status();
 }
 

@@ -116,7 +116,8 @@ struct VisibleRows {
   __device__ bool full(int unit) const {
     return unit * 16 + 16 <= len && (unit * 16 >= first || unit * 16 + 16 <= n_sink);
   }
-  __device__ bool sees(int j) const { return j < len && (j >= first || j < n_sink); }
+  // (without a branch: with one, the compiler left scores of rows in front of a window as they were)
+  __device__ bool sees(int j) const { return (j < len) & ((j >= first) | (j < n_sink)); }
 };
 
 __device__ inline f32x4_t mfma_bf16(uint4 a, uint4 b, f32x4_t c) {
@@ -188,9 +189,9 @@ struct PagedTile<bf16_t, DP> {
         }
       }
   }
-  __device__ void drop_v(int e) {
+  __device__ void keep_v(int e, bool seen) {
 #pragma unroll
-    for (int w = 0; w < kE / 2 * kLoads; ++w) v[e][w] = 0;
+    for (int w = 0; w < kE / 2 * kLoads; ++w) v[e][w] = seen ? v[e][w] : 0;
   }
   __device__ void scores(float* x) const {
 #pragma unroll
@@ -245,9 +246,11 @@ struct PagedTile<float, DP> {
       for (int l = 0; l < DP / 64; ++l)
         v[r][l] = *(const f32x4_t*)(base + (unsigned)((4 * g + r) * d + min(64 * l + 4 * c, d - 4)) * 4u);
   }
-  __device__ void drop_v(int e) {
+  __device__ void keep_v(int e, bool seen) {
 #pragma unroll
-    for (int l = 0; l < DP / 64; ++l) v[e][l] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int l = 0; l < DP / 64; ++l)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[e][l][i] = seen ? v[e][l][i] : 0.f;
   }
   __device__ void scores(float* x) const {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
@@ -339,11 +342,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(c
     for (int u = 0; u < kU; ++u) full = full && at[u] >= 0 && rows.full(rows.unit(u0 + u));
     if (!full) {
 #pragma unroll
-      for (int e = 0; e < Tile::kScores; ++e)
-        if (at[e / 4] < 0 || !rows.sees(rows.unit(u0 + e / 4) * 16 + 4 * g + e % 4)) {
-          x[e] = -INFINITY;
-          tile.drop_v(e);
-        }
+      for (int e = 0; e < Tile::kScores; ++e) {
+        const bool seen = rows.sees(rows.unit(u0 + e / 4) * 16 + 4 * g + e % 4) & (at[e / 4] >= 0);
+        x[e] = seen ? x[e] : -INFINITY;
+        tile.keep_v(e, seen);
+      }
     }
     float top = x[0];
 #pragma unroll

@@ -70,6 +70,8 @@ __device__ inline double wave_sum_f64(double v) {
   return v;
 }
 
+__device__ inline float mass_of(float p) { return p > 0.f ? p : 0.f; }       // (a NaN has none)
+
 // What is left of a row: the part of column i that a draw can still hit.
 struct RestOfRow {
   const float *p, *q;        // q: NULL where the children were chosen
@@ -77,7 +79,7 @@ struct RestOfRow {
   const int* refused;        // LDS: columns that do not count
   int n_refused;
   __device__ double at(int i) const {
-    const double v = (double)p[i] - (q ? less * (double)q[i] : 0.0);
+    const double v = (double)p[i] - (q ? less * (double)mass_of(q[i]) : 0.0);
     if (!(v > 0.0)) return 0.0;                    // (a NaN too)
     for (int r = 0; r < n_refused; ++r)
       if (refused[r] == i) return 0.0;
@@ -184,8 +186,8 @@ __global__ __launch_bounds__(NT) void sampled_accept_kernel(const SampleArgs a) 
     s_parent[c] = par;
     s_col[c] = in ? (int)col : -1;
     s_u[c] = a.u_accept[base + c];
-    s_p[c] = in ? a.target[(base + par) * n + col] : 0.f;
-    s_q[c] = in && a.draft ? a.draft[(base + par) * n + col] : 0.f;
+    s_p[c] = in ? mass_of(a.target[(base + par) * n + col]) : 0.f;
+    s_q[c] = in && a.draft ? mass_of(a.draft[(base + par) * n + col]) : 0.f;
     a.accept_mask[base + c] = c == 0;
   }
   for (int i = tid; i <= a.d_cap; i += NT) {

@@ -58,6 +58,8 @@ class VerifyPass:
         self.best_node = torch.zeros(self.B, dtype=torch.int32, device=device)
         self.path = torch.zeros(self.B, self.d_cap + 1, dtype=torch.int32, device=device)
         self.out_tokens = torch.zeros(self.B, self.d_cap + 1, dtype=torch.int32, device=device)
+        self.probs: Optional[torch.Tensor] = None             # of accept_sampled(), with its status
+        self.accept_status: Optional[torch.Tensor] = None
 
     # ---- loading -------------------------------------------------------------------
     def load_layer(self, layer: int, raw: Dict[str, torch.Tensor]) -> None:
@@ -134,6 +136,20 @@ class VerifyPass:
                              self.wc.action_lo, self.wc.n_bins, r, self.B, self.d_cap,
                              self.accept_mask, self.accepted_len, self.best_node, self.path,
                              self.out_tokens)
+
+    def accept_sampled(self, u_accept: torch.Tensor, u_draw: torch.Tensor, temperature: float = 1.0,
+                       draft_prob: Optional[torch.Tensor] = None) -> None:
+        """Acceptance that keeps the verifier's distribution at this temperature, from the logits of the last
+        forward(want_logits=True) and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
+        [B*T, scored tokens] where the drafter drew its tokens.  Leaves what accept() leaves, so that
+        commit() follows; accept_status is not 0 where an episode had nothing to draw from."""
+        if self.probs is None:
+            self.probs = torch.empty_like(self.logits)
+            self.accept_status = torch.zeros(self.B, dtype=torch.int32, device=self.device)
+        sv.sv_token_probs(self.logits, temperature, self.probs)
+        sv.sv_sampled_accept(self.tree.struct, self.draft, self.probs, draft_prob, self.vocab_lo, u_accept, u_draw,
+                             self.B, self.d_cap, self.accept_mask, self.accepted_len, self.best_node, self.path,
+                             self.out_tokens, self.accept_status)
 
     def step(self, r: int, want_logits: bool = False, head: str = "auto") -> None:
         self.forward(want_logits=want_logits, head=head)

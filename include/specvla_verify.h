@@ -376,7 +376,7 @@ int sv_sampled_accept(const sv_tree *tree, const int32_t *draft_token, const flo
 #define SV_MAX_PAGED_HEAD_DIM 256
 typedef struct sv_paged_cache {
   void *k, *v;                /* [device] [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned */
-  const int32_t *block_table; /* [device] int32 [n_seqs][max_pages]; entries behind a sequence's last page are not read */
+  const int32_t *block_table; /* [device] int32 [n_seqs][max_pages]; entries behind a sequence's last page are not used */
   int32_t dtype;              /* SV_F32 or SV_BF16 (the cache of 8-bit and 4-bit weight models too) */
   int32_t n_seqs, max_pages, n_pages;
   int32_t page_size;          /* a multiple of 16 */

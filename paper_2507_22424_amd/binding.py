@@ -444,22 +444,41 @@ def sv_tree_build_device(cand_parent: torch.Tensor, cand_logp: torch.Tensor, can
         _dev(status, torch.int32, "status"), _stream(stream)), "sv_tree_build_device")
 
 
-def _one_device(**tensors) -> None:
-    """The tensors of a call lie on the device that it is launched on, the current one."""
-    current = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for name, t in tensors.items():
-        if t is not None and t.device.index != current:
-            raise ValueError(f"{name} is on {t.device}, the current device is {current}")
+# The calls below are short on the GPU, so that their arguments are looked over in one go: a tensor lies on the device
+# that the call is launched on, has the type, and is contiguous.
+_get_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _device() -> int:
+    return torch.cuda.current_device() if _get_device is None or not torch.cuda.is_initialized() else _get_device()
+
+
+def _stream_on(stream, device: int) -> int:
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
+
+
+def _ptr(t: torch.Tensor, dtype: torch.dtype, device: int, name: str) -> int:
+    if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the current device {device}, got {t.dtype} on "
+                         f"{t.device} with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _opt(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, name: str) -> Optional[int]:
+    return None if t is None else _ptr(t, dtype, device, name)
+
+
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
 def sv_token_probs(logits: torch.Tensor, temperature: float, probs: torch.Tensor, stream=None) -> None:
     """probs = softmax(logits / temperature) of [rows, vocabulary]; `probs` may be `logits`."""
     if logits.dim() != 2 or probs.shape != logits.shape:
         raise ValueError("token_probs: logits and probs must be [rows, vocabulary]")
-    args = (_dev(logits, torch.float32, "logits"), logits.shape[0], logits.shape[1], temperature,
-            _dev(probs, torch.float32, "probs"))
-    _one_device(logits=logits, probs=probs)
-    _check(lib().sv_token_probs(*args, _stream(stream)), "sv_token_probs")
+    dev = _device()
+    rc = lib().sv_token_probs(_ptr(logits, _F32, dev, "logits"), *logits.shape, temperature, _ptr(probs, _F32, dev, "probs"),
+                              _stream_on(stream, dev))
+    _check(rc, "sv_token_probs")
 
 
 def sv_sampled_accept(tree: Tree, draft_token: torch.Tensor, target_prob: torch.Tensor,
@@ -467,51 +486,52 @@ def sv_sampled_accept(tree: Tree, draft_token: torch.Tensor, target_prob: torch.
                       u_draw: torch.Tensor, B: int, d_cap: int, accept_mask: torch.Tensor,
                       accepted_len: torch.Tensor, best_node: torch.Tensor, path: torch.Tensor,
                       out_tokens: torch.Tensor, status: torch.Tensor, stream=None) -> None:
-    T = tree.n_nodes
-    n_vocab = target_prob.shape[-1]
-    if target_prob.numel() != B * T * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
-            draft_token.numel() != B * T or u_accept.numel() != B * T or u_draw.numel() != B or \
-            accept_mask.numel() != B * T or accepted_len.numel() != B or best_node.numel() != B or \
-            status.numel() != B or path.numel() != B * (d_cap + 1) or out_tokens.numel() != B * (d_cap + 1):
+    """target_prob, draft_prob: [B*T, columns]; the other sizes as in sv_relaxed_accept."""
+    n, n_vocab = B * tree.n_nodes, target_prob.shape[-1]
+    if target_prob.numel() != n * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
+            draft_token.numel() != n or u_accept.numel() != n or u_draw.numel() != B or accept_mask.numel() != n or \
+            accepted_len.numel() != B or best_node.numel() != B or status.numel() != B or \
+            path.numel() != B * (d_cap + 1) or out_tokens.numel() != B * (d_cap + 1):
         raise ValueError("sampled_accept: tensor sizes do not match B, T, d_cap")
-    args = (_dev(draft_token, torch.int32, "draft_token"), _dev(target_prob, torch.float32, "target_prob"),
-            _dev(draft_prob, torch.float32, "draft_prob"), n_vocab, vocab_lo, _dev(u_accept, torch.float32, "u_accept"),
-            _dev(u_draw, torch.float32, "u_draw"), B, d_cap, _dev(accept_mask, torch.uint8, "accept_mask"),
-            _dev(accepted_len, torch.int32, "accepted_len"), _dev(best_node, torch.int32, "best_node"),
-            _dev(path, torch.int32, "path"), _dev(out_tokens, torch.int32, "out_tokens"), _dev(status, torch.int32, "status"))
-    _one_device(target_prob=target_prob, draft_prob=draft_prob, draft_token=draft_token, u_accept=u_accept, u_draw=u_draw,
-                accept_mask=accept_mask, accepted_len=accepted_len, best_node=best_node, path=path,
-                out_tokens=out_tokens, status=status)
-    _check(lib().sv_sampled_accept(C.byref(tree), *args, _stream(stream)), "sv_sampled_accept")
+    dev = _device()
+    rc = lib().sv_sampled_accept(
+        C.byref(tree), _ptr(draft_token, _I32, dev, "draft_token"), _ptr(target_prob, _F32, dev, "target_prob"),
+        _opt(draft_prob, _F32, dev, "draft_prob"), n_vocab, vocab_lo, _ptr(u_accept, _F32, dev, "u_accept"),
+        _ptr(u_draw, _F32, dev, "u_draw"), B, d_cap, _ptr(accept_mask, _U8, dev, "accept_mask"),
+        _ptr(accepted_len, _I32, dev, "accepted_len"), _ptr(best_node, _I32, dev, "best_node"), _ptr(path, _I32, dev, "path"),
+        _ptr(out_tokens, _I32, dev, "out_tokens"), _ptr(status, _I32, dev, "status"), _stream_on(stream, dev))
+    _check(rc, "sv_sampled_accept")
 
 
-def _token_rows(t: Optional[torch.Tensor], n_tokens: int, heads: Optional[int], d: int, name: str) -> Tuple[int, int, int]:
-    """(pointer, heads, stride in elements) of [tokens, heads, d] whose tokens may lie apart."""
-    if t is None:
-        return 0, 0, 0
-    if not t.is_cuda or t.dtype != torch.float32:
-        raise ValueError(f"{name} must be a float32 device tensor")
-    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != d or (heads is not None and t.shape[1] != heads) or \
-            t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
-        raise ValueError(f"{name} must be [{n_tokens}, {heads or 'heads'}, {d}] with contiguous tokens")
-    return t.data_ptr(), t.shape[1], t.stride(0) if n_tokens > 1 else t.shape[1] * d
+def _token_rows(t: torch.Tensor, n: int, heads: int, d: int, device: int, name: str) -> Tuple[int, int]:
+    """(pointer, elements from token to token) of float32 [n, heads, d] whose tokens may lie apart."""
+    if t.get_device() != device or t.dtype is not _F32 or t.shape != (n, heads, d):
+        raise ValueError(f"{name} must be a {_F32} tensor [{n}, {heads}, {d}] on the current device {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    a, b, c = t.stride()
+    if c != 1 or (heads > 1 and b != d):
+        raise ValueError(f"the heads of a token of {name} must be contiguous, got strides {t.stride()}")
+    return t.data_ptr(), a if n > 1 else heads * d
 
 
 def sv_paged_append(cache: "PagedCache", token_seq: torch.Tensor, token_pos: torch.Tensor, q: Optional[torch.Tensor],
                     k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor], rope_theta: float,
                     status: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, k, v: [tokens, heads, head_dim] float32, views of a fused projection among them."""
-    n, c = token_seq.numel(), cache.struct
+    n, c, dev = token_seq.numel(), cache.struct, _device()
+    nkv, d = c.n_kv_heads, c.head_dim
     if token_pos.numel() != n or (status is not None and status.numel() != n) or (q is None) != (q_out is None) or \
-            (q is not None and q_out.shape != q.shape):
+            (q is not None and (q.dim() != 3 or q_out.shape != q.shape)):
         raise ValueError("paged_append: tensor sizes do not match the tokens")
-    qp, n_q, q_stride = _token_rows(q, n, None, c.head_dim, "q")
-    kp, _, k_stride = _token_rows(k, n, c.n_kv_heads, c.head_dim, "k")
-    vp, _, v_stride = _token_rows(v, n, c.n_kv_heads, c.head_dim, "v")
-    args = (n, _dev(token_seq, torch.int32, "token_seq"), _dev(token_pos, torch.int32, "token_pos"), qp, n_q, q_stride,
-            kp, k_stride, vp, v_stride, rope_theta, _dev(q_out, torch.float32, "q_out"), _dev(status, torch.int32, "status"))
-    _one_device(cache=cache.k, token_seq=token_seq, token_pos=token_pos, q=q, k=k, v=v, q_out=q_out, status=status)
-    _check(lib().sv_paged_append(C.byref(c), *args, _stream(stream)), "sv_paged_append")
+    nq = 0 if q is None else q.shape[1]
+    qp, q_stride = (None, 0) if q is None else _token_rows(q, n, nq, d, dev, "q")
+    kp, k_stride = _token_rows(k, n, nkv, d, dev, "k")
+    vp, v_stride = _token_rows(v, n, nkv, d, dev, "v")
+    cache.check_device(dev)
+    rc = lib().sv_paged_append(C.byref(c), n, _ptr(token_seq, _I32, dev, "token_seq"), _ptr(token_pos, _I32, dev, "token_pos"),
+                               qp, nq, q_stride, kp, k_stride, vp, v_stride, rope_theta, _opt(q_out, _F32, dev, "q_out"),
+                               _opt(status, _I32, dev, "status"), _stream_on(stream, dev))
+    _check(rc, "sv_paged_append")
 
 
 def sv_paged_workspace_bytes(cache: "PagedCache", n_q_heads: int, max_len: int) -> int:
@@ -525,16 +545,18 @@ def sv_paged_attention(cache: "PagedCache", seq_len: torch.Tensor, max_len: int,
                        window: int, n_sink: int, out: torch.Tensor, lse: Optional[torch.Tensor],
                        status: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     """q, out: [sequences, query heads, head_dim] float32; window 0: every row is visible."""
-    c = cache.struct
-    if q.dim() != 3 or q.shape[0] != c.n_seqs or q.shape[2] != c.head_dim or out.shape != q.shape or \
-            seq_len.numel() != c.n_seqs or (lse is not None and lse.numel() != c.n_seqs * q.shape[1]) or \
-            (status is not None and status.numel() != c.n_seqs):
+    c, dev = cache.struct, _device()
+    n_seqs = c.n_seqs
+    if q.dim() != 3 or q.shape[0] != n_seqs or q.shape[2] != c.head_dim or out.shape != q.shape or \
+            seq_len.numel() != n_seqs or (lse is not None and lse.numel() != n_seqs * q.shape[1]) or \
+            (status is not None and status.numel() != n_seqs):
         raise ValueError("paged_attention: tensor sizes do not match the cache")
-    args = (_dev(seq_len, torch.int32, "seq_len"), max_len, _dev(q, torch.float32, "q"), q.shape[1], scale, window, n_sink,
-            _dev(out, torch.float32, "out"), _dev(lse, torch.float32, "lse"), _dev(status, torch.int32, "status"),
-            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
-    _one_device(cache=cache.k, seq_len=seq_len, q=q, out=out, lse=lse, status=status, workspace=workspace)
-    _check(lib().sv_paged_attention(C.byref(c), *args, _stream(stream)), "sv_paged_attention")
+    cache.check_device(dev)
+    rc = lib().sv_paged_attention(
+        C.byref(c), _ptr(seq_len, _I32, dev, "seq_len"), max_len, _ptr(q, _F32, dev, "q"), q.shape[1], scale, window, n_sink,
+        _ptr(out, _F32, dev, "out"), _opt(lse, _F32, dev, "lse"), _opt(status, _I32, dev, "status"),
+        _ptr(workspace, _U8, dev, "workspace"), workspace.numel(), _stream_on(stream, dev))
+    _check(rc, "sv_paged_attention")
 
 
 # ---- holders that keep the device tensors behind the C structs alive -------------------
@@ -585,6 +607,11 @@ class PagedCache:
         self.struct = PagedView(_dev(k, name="k"), _dev(v, name="v"), _dev(block_table, torch.int32, "block_table"),
                                 SV_F32 if k.dtype == torch.float32 else SV_BF16, block_table.shape[0],
                                 block_table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3])
+        self.device = k.get_device()
+
+    def check_device(self, device: int) -> None:
+        if self.device != device:
+            raise ValueError(f"the cache lies on device {self.device}, the current device is {device}")
 
     @classmethod
     def of_kv_cache(cls, kv: "KvCache") -> "PagedCache":

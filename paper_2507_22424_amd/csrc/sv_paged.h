@@ -142,35 +142,42 @@ __device__ inline void split8_3(const float* v, uint4* part) {
   }
 }
 
+// A load of the cache; NT: past the caches.
+template <int NT, typename V>
+__device__ inline V load_row(const char* p) {
+  typedef unsigned words_t __attribute__((ext_vector_type(sizeof(V) / 4)));
+  const auto src = (const __attribute__((address_space(1))) words_t*)p;
+  if constexpr (NT) return __builtin_bit_cast(V, __builtin_nontemporal_load(src));
+  else return __builtin_bit_cast(V, *src);
+}
+
 // A tile of the cache in registers and its two products.  DP: head_dim rounded up to 64, 128 or 256 (columns
 // behind head_dim: q is zero, K and V repeat columns of the row, and the outputs are not stored).
-template <typename T, int DP>
+template <typename T, int DP, int NT>
 struct PagedTile;
 
-template <int DP>
-struct PagedTile<bf16_t, DP> {
+template <int DP, int NT>
+struct PagedTile<bf16_t, DP, NT> {
   static constexpr int kUnits = 2, kSteps = DP / 32, kOut = DP / 16;
   static constexpr int kE = DP / 16 < 8 ? DP / 16 : 8, kLoads = DP / 16 / kE;    // V: elements of a load, loads of a row
   static constexpr int kScores = 8;
   uint4 k[2][kSteps];
   uint32_t v[8][kE / 2 * kLoads];
-  uint4 q[kSteps][3];
+  typedef uint4 QPart;
+  static constexpr int kParts = 3;           // of the query operand of a step
 
   static __device__ int out_col(int t, int m) { return t / kE * 16 * kE + kE * m + t % kE; }
-  __device__ void load_q(const float* src, bool real, float scale, int d, int g) {
+  static __device__ void load_q(int s, const float* src, bool real, float scale, int d, int g, QPart* part) {
+    float x[8];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = real && 32 * s + 8 * g < d ? src[32 * s + 8 * g + e] * scale : 0.f;
-      split8_3(x, q[s]);
-    }
+    for (int e = 0; e < 8; ++e) x[e] = real && 32 * s + 8 * g < d ? src[32 * s + 8 * g + e] * scale : 0.f;
+    split8_3(x, part);
   }
   __device__ void load_k(int u, const char* base, int d, int g, int c) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int col = min(32 * s + 8 * g, d - 8);
-      k[u][s] = *(const uint4*)(base + (unsigned)(c * d + col) * 2u);
+      k[u][s] = load_row<NT, uint4>(base + (unsigned)(c * d + col) * 2u);
     }
   }
   __device__ void load_v(int u, const char* base, int d, int g, int c) {
@@ -181,10 +188,10 @@ struct PagedTile<bf16_t, DP> {
         const char* p = base + (unsigned)((4 * g + r) * d + min(128 * l + kE * c, d - kE)) * 2u;
         uint32_t* dst = v[4 * u + r] + l * (kE / 2);
         if constexpr (kE == 8) {
-          const uint4 w = *(const uint4*)p;
+          const uint4 w = load_row<NT, uint4>(p);
           dst[0] = w.x; dst[1] = w.y; dst[2] = w.z; dst[3] = w.w;
         } else {
-          const uint2 w = *(const uint2*)p;
+          const uint2 w = load_row<NT, uint2>(p);
           dst[0] = w.x; dst[1] = w.y;
         }
       }
@@ -193,17 +200,19 @@ struct PagedTile<bf16_t, DP> {
 #pragma unroll
     for (int w = 0; w < kE / 2 * kLoads; ++w) v[e][w] = seen ? v[e][w] : 0;
   }
-  __device__ void scores(float* x) const {
+  // q: LDS, [part][64 lanes]
+  __device__ void scores(const QPart (*q)[64], int lane, float* x) const {
+    f32x4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 2; p >= 0; --p)
 #pragma unroll
-      for (int p = 0; p < 3; ++p)
+      for (int i = 0; i < kSteps; ++i) {
+        const uint4 w = q[3 * i + p][lane];
+        s[0] = mfma_bf16(k[0][i], w, s[0]);
+        s[1] = mfma_bf16(k[1][i], w, s[1]);
+      }
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) s = mfma_bf16(k[u][i], q[i][2 - p], s);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[4 * u + r] = s[r];
-    }
+    for (int e = 0; e < 8; ++e) x[e] = s[e / 4][e % 4];
   }
   __device__ void add(const float* p, f32x4_t* o) const {
     uint4 w[3];
@@ -222,29 +231,29 @@ struct PagedTile<bf16_t, DP> {
   }
 };
 
-template <int DP>
-struct PagedTile<float, DP> {
+template <int DP, int NT>
+struct PagedTile<float, DP, NT> {
   static constexpr int kUnits = 1, kSteps = DP / 16, kOut = DP / 16;
   static constexpr int kScores = 4;
-  f32x4_t k[1][kSteps], v[4][DP / 64], q[kSteps];
+  f32x4_t k[1][kSteps], v[4][DP / 64];
+  typedef f32x4_t QPart;
+  static constexpr int kParts = 1;
 
   static __device__ int out_col(int t, int m) { return t / 4 * 64 + 4 * m + t % 4; }
-  __device__ void load_q(const float* src, bool real, float scale, int d, int g) {
+  static __device__ void load_q(int s, const float* src, bool real, float scale, int d, int g, QPart* part) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q[s][e] = real && 16 * s + 4 * g < d ? src[16 * s + 4 * g + e] * scale : 0.f;
+    for (int e = 0; e < 4; ++e) part[0][e] = real && 16 * s + 4 * g < d ? src[16 * s + 4 * g + e] * scale : 0.f;
   }
   __device__ void load_k(int, const char* base, int d, int g, int c) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[0][s] = *(const f32x4_t*)(base + (unsigned)(c * d + min(16 * s + 4 * g, d - 4)) * 4u);
+    for (int s = 0; s < kSteps; ++s) k[0][s] = load_row<NT, f32x4_t>(base + (unsigned)(c * d + min(16 * s + 4 * g, d - 4)) * 4u);
   }
   __device__ void load_v(int, const char* base, int d, int g, int c) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int l = 0; l < DP / 64; ++l)
-        v[r][l] = *(const f32x4_t*)(base + (unsigned)((4 * g + r) * d + min(64 * l + 4 * c, d - 4)) * 4u);
+        v[r][l] = load_row<NT, f32x4_t>(base + (unsigned)((4 * g + r) * d + min(64 * l + 4 * c, d - 4)) * 4u);
   }
   __device__ void keep_v(int e, bool seen) {
 #pragma unroll
@@ -252,12 +261,14 @@ struct PagedTile<float, DP> {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[e][l][i] = seen ? v[e][l][i] : 0.f;
   }
-  __device__ void scores(float* x) const {
+  __device__ void scores(const QPart (*q)[64], int lane, float* x) const {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i) {
+      const f32x4_t w = q[i][lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[i][e], s, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], w[e], s, 0, 0, 0);
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] = s[r];
   }
@@ -269,81 +280,92 @@ struct PagedTile<float, DP> {
   }
 };
 
-// One workgroup = (sequence, KV head, block of 16 query heads, split); its four waves take tiles in turn.
-// grid.x = sequences * KV heads * splits * blocks.
-template <typename T, int DP>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(const PagedAttnArgs a) {
-  using Tile = PagedTile<T, DP>;
-  constexpr int kU = Tile::kUnits, kPitch = DP + 4;
-  __shared__ float s_m[4][16], s_l[4][16];
-  __shared__ __attribute__((aligned(16))) float s_o[4][16][kPitch];
+// One workgroup = (sequence, KV head, block of 16 query heads, split); its four waves take tiles in turn.  A lane of a
+// wave looks up the page of one of the wave's units, all of them before the first is needed: a split has at most
+// kBatchUnits of them per wave.  grid.x = sequences * KV heads * splits, rounded up to a multiple of 8, * blocks.
+constexpr int kBatchUnits = 64, kPagedWaves = 4;
+template <typename T, int DP, int NT>
+__global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_attention_mfma(const PagedAttnArgs a) {
+  using Tile = PagedTile<T, DP, NT>;
+  constexpr int kU = Tile::kUnits, kPitch = DP + 4, NW = kPagedWaves;
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ __attribute__((aligned(16))) float s_o[NW][16][kPitch];
+  __shared__ typename Tile::QPart s_q[Tile::kSteps * Tile::kParts][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15, d = a.c.d;
-  unsigned id = blockIdx.x;
-  const int hb = id % a.n_blocks;
-  id /= a.n_blocks;
-  const int split = id % a.n_split;
-  id /= a.n_split;
-  const int hk = id % a.c.n_kv, seq = id / a.c.n_kv;
-  const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
-  const int u_begin = split * a.split_units, u_end = min(rows.n_units, u_begin + a.split_units);
-  if (u_begin >= u_end && split > 0) return;
+  // Workgroups go to the XCDs in turn.  Heads come first and splits last: with the splits first, an XCD got one split of
+  // every sequence, and those of the last splits, which only long sequences have, little to do.  The blocks of a KV
+  // head's queries, which read the same rows, go to one XCD, one right after the other.
+  const unsigned octet = blockIdx.x / (8 * a.n_blocks), in_octet = blockIdx.x % (8 * a.n_blocks);
+  const int hb = in_octet / 8;
+  unsigned id = octet * 8 + in_octet % 8;
+  const int hk = id % a.c.n_kv;
+  id /= a.c.n_kv;
+  const int seq = id % a.c.n_seqs, split = a.n_split - 1 - (int)(id / a.c.n_seqs);
+  if (split < 0) return;            // (the tasks are rounded up to a multiple of 8)
+  const int u_begin = split * a.split_units, u_wave = u_begin + wave * kU;
   const int G = a.n_q / a.c.n_kv, n_heads = min(16, G - 16 * hb);
   const size_t row0 = (size_t)seq * a.n_q + hk * G + 16 * hb;
 
+  // The first loads - length, pages of the units, queries - do not wait for each other: without a window the units
+  // are known before the length is (pages of units behind it are looked up too, and not used).
+  const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
+  const int my_unit = u_wave + lane / kU * (NW * kU) + lane % kU;
+  const int my_at = a.window ? rows.unit(my_unit) : my_unit, page_units = a.c.page_size / 16, my_page = my_at / page_units;
+  const int page = a.c.table[(size_t)seq * a.c.max_pages + min(my_page, a.c.max_pages - 1)];
+  const bool in_pool = (unsigned)page < (unsigned)a.c.n_pages;
+  const long long my_off = in_pool ? (((long long)page * a.c.n_kv + hk) * a.c.page_size + (my_at - my_page * page_units) * 16) * d * (int)sizeof(T) : 0;
   Tile tile;
-  tile.load_q(a.q + (row0 + c) * d, c < n_heads, a.scale, d, g);
+  typename Tile::QPart part[Tile::kSteps / NW + 1][Tile::kParts];
+#pragma unroll
+  for (int s = 0; s * NW < Tile::kSteps; ++s)
+    if (s * NW + wave < Tile::kSteps)
+      Tile::load_q(s * NW + wave, a.q + (row0 + min(c, n_heads - 1)) * d, c < n_heads, a.scale, d, g, part[s]);
+  const unsigned long long pool_units = __builtin_amdgcn_ballot_w64(in_pool);
+  auto offset = [&](int i) {                 // bytes of the wave's i-th unit
+    return (size_t)(unsigned)__builtin_amdgcn_readlane((int)my_off, i) | (size_t)__builtin_amdgcn_readlane((int)(my_off >> 32), i) << 32;
+  };
+  auto load_k = [&](int it) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) tile.load_k(u, (const char*)a.c.k + offset(it * kU + u), d, g, c);
+  };
+  auto load_v = [&](int it) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) tile.load_v(u, (const char*)a.c.v + offset(it * kU + u), d, g, c);
+  };
+  load_k(0);
+  load_v(0);
+
+#pragma unroll
+  for (int s = 0; s * NW < Tile::kSteps; ++s)
+    if (s * NW + wave < Tile::kSteps)
+#pragma unroll
+      for (int p = 0; p < Tile::kParts; ++p) s_q[(s * NW + wave) * Tile::kParts + p][lane] = part[s][p];
+  const int u_end = min(rows.n_units, u_begin + a.split_units);
+  __syncthreads();
+  if (u_begin >= u_end && split > 0) return;
+  const int n_it = max(0, u_end - u_wave + NW * kU - 1) / (NW * kU);
   f32x4_t o[Tile::kOut];
 #pragma unroll
   for (int t = 0; t < Tile::kOut; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  bool bad = false;
-
-  const int32_t* table = a.c.table + (size_t)seq * a.c.max_pages;
-  const int page_units = a.c.page_size / 16;
-  // where unit u of this sequence lies: offset in bytes, -1 where its page is none
-  auto locate = [&](int u) -> long long {
-    if (u >= u_end) return -1;
-    const int at = rows.unit(u), p = at / page_units;
-    const int page = __builtin_amdgcn_readfirstlane(table[p]);
-    if ((unsigned)page >= (unsigned)a.c.n_pages) {
-      bad = true;
-      return -1;
-    }
-    return (((long long)page * a.c.n_kv + hk) * a.c.page_size + (at - p * page_units) * 16) * d * (long long)sizeof(T);
-  };
-  long long at[kU], next[kU];
-  auto load_k = [&](const long long* w) {
-#pragma unroll
-    for (int u = 0; u < kU; ++u) tile.load_k(u, (const char*)a.c.k + (w[u] < 0 ? 0 : w[u]), d, g, c);
-  };
-  auto load_v = [&](const long long* w) {
-#pragma unroll
-    for (int u = 0; u < kU; ++u) tile.load_v(u, (const char*)a.c.v + (w[u] < 0 ? 0 : w[u]), d, g, c);
-  };
-  int u0 = u_begin + wave * kU;
-  if (u0 < u_end) {
-#pragma unroll
-    for (int u = 0; u < kU; ++u) at[u] = locate(u0 + u);
-    load_k(at);
-    load_v(at);
-  }
-  for (; u0 < u_end; u0 += 4 * kU) {
+  for (int it = 0; it < n_it; ++it) {
     float x[Tile::kScores];
-    tile.scores(x);
-    const bool more = u0 + 4 * kU < u_end;
-    if (more) {
-#pragma unroll
-      for (int u = 0; u < kU; ++u) next[u] = locate(u0 + 4 * kU + u);
-      load_k(next);
-    }
+    int q_lane = lane;
+    asm volatile("" : "+v"(q_lane));         // (else the queries are taken out of the loop, into registers)
+    tile.scores(s_q, q_lane, x);
+    const bool more = it + 1 < n_it;
+    if (more) load_k(it + 1);
+    const int u0 = u_wave + it * (NW * kU);
     bool full = true;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) full = full && at[u] >= 0 && rows.full(rows.unit(u0 + u));
+    for (int u = 0; u < kU; ++u)
+      full = full & (u0 + u < u_end) & (bool)(pool_units >> (it * kU + u) & 1) & rows.full(rows.unit(u0 + u));
     if (!full) {
 #pragma unroll
       for (int e = 0; e < Tile::kScores; ++e) {
-        const bool seen = rows.sees(rows.unit(u0 + e / 4) * 16 + 4 * g + e % 4) & (at[e / 4] >= 0);
+        const int u = e / 4;
+        const bool seen = rows.sees(rows.unit(u0 + u) * 16 + 4 * g + e % 4) & (u0 + u < u_end) & (bool)(pool_units >> (it * kU + u) & 1);
         x[e] = seen ? x[e] : -INFINITY;
         tile.keep_v(e, seen);
       }
@@ -371,9 +393,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(c
       l += p[e];
     }
     tile.add(p, o);
-    if (more) load_v(next);
-#pragma unroll
-    for (int u = 0; u < kU; ++u) at[u] = next[u];
+    if (more) load_v(it + 1);
   }
 
   // ---- join the waves ----
@@ -390,14 +410,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(c
       for (int r = 0; r < 4; ++r) s_o[wave][c][Tile::out_col(t, 4 * g + r)] = o[t][r];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n_heads * (d / 4); i += 256) {
+  for (int i = threadIdx.x; i < n_heads * (d / 4); i += 64 * NW) {
     const int h = i / (d / 4), e = (i - h * (d / 4)) * 4;
     float m_all = -INFINITY, l_all = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, s_m[w][h]);
+    for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, s_m[w][h]);
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float f = s_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][h] - m_all);
       l_all += f * s_l[w][h];
       v += f * *(const f32x4_t*)&s_o[w][h][e];
@@ -415,42 +435,88 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void paged_attention_mfma(c
       if (e == 0 && a.lse) a.lse[row] = l_all == 0.f ? -INFINITY : (m_all + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
     }
   }
-  if (a.status && hk == 0 && hb == 0) {
-    // (one wave sees a bad page at least where there is one)
-    if (a.n_split == 1) {
-      const int any = __syncthreads_or(bad);
-      if (threadIdx.x == 0) a.status[seq] = any;
-    }
+  if (a.status && a.n_split == 1 && hk == 0 && hb == 0) {
+    const int any = __syncthreads_or(!in_pool & (my_unit < u_end));
+    if (threadIdx.x == 0) a.status[seq] = any;
   }
 }
 
-// Joins the splits of a row in their order; one wave looks over the pages of a sequence for the status.
-// grid = (query heads, sequences), block = 256.
-__global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs a) {
-  const int h = blockIdx.x, seq = blockIdx.y, d = a.c.d;
-  const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
-  const int n = max(1, (rows.n_units + a.split_units - 1) / a.split_units);
-  const size_t row = (size_t)seq * a.n_q + h;
-  const float* ml = a.part_ml + row * a.n_split * 2;
-  const float* part = a.part + row * a.n_split * d;
-  float m = -INFINITY, l = 0.f, v = 0.f;
-  for (int s = 0; s < n; ++s) m = fmaxf(m, ml[2 * s]);
-  for (int s = 0; s < n; ++s) {
-    const float f = ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2 * s] - m);
-    l += f * ml[2 * s + 1];
-    if ((int)threadIdx.x < d) v += f * part[(size_t)s * d + threadIdx.x];
-  }
-  if ((int)threadIdx.x < d) a.out[row * d + threadIdx.x] = l != 0.f ? v / l : 0.f;
-  if (threadIdx.x == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  if (a.status && h == 0) {
+// Joins the splits of a row.  A thread has four columns of it and every J-th split; the J sums are added in order
+// through LDS.  J = 1 up to eight splits, whose loads a thread has under way together.  Behind the workgroups that
+// join (grid: ceil(rows * d / 4 / (256 / J))) come one per sequence that look over its pages for the status.
+template <int J>
+__global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs a, unsigned n_join) {
+  constexpr int kCols = 256 / J;             // columns (of four) of a workgroup
+  __shared__ float s_l[J][kCols];
+  __shared__ f32x4_t s_v[J][kCols];
+  const int d = a.c.d, tid = threadIdx.x, quads = d / 4;
+  if (blockIdx.x >= n_join) {
+    const int seq = blockIdx.x - n_join, page_units = a.c.page_size / 16;
+    const VisibleRows rows(a.seq_len[seq], a.max_len, a.window, a.n_sink);
     bool bad = false;
-    for (int u = threadIdx.x; u < rows.n_units; u += 256) {
-      const int page = a.c.table[(size_t)seq * a.c.max_pages + rows.unit(u) / (a.c.page_size / 16)];
-      bad |= (unsigned)page >= (unsigned)a.c.n_pages;
-    }
+    for (int u = tid; u < rows.n_units; u += 256)
+      bad |= (unsigned)a.c.table[(size_t)seq * a.c.max_pages + rows.unit(u) / page_units] >= (unsigned)a.c.n_pages;
     const int any = __syncthreads_or(bad);
-    if (threadIdx.x == 0) a.status[seq] = any;
+    if (tid == 0) a.status[seq] = any;
+    return;
   }
+  const unsigned n_rows = (unsigned)a.c.n_seqs * a.n_q;
+  const size_t at = (size_t)blockIdx.x * kCols + tid % kCols;
+  const unsigned row = min((unsigned)(at / quads), n_rows - 1);
+  const int col = (int)(at % quads) * 4, i = tid / kCols;
+  const bool real = at < (size_t)n_rows * quads;
+  const VisibleRows rows(a.seq_len[row / a.n_q], a.max_len, a.window, a.n_sink);
+  const int n = max(1, (rows.n_units + a.split_units - 1) / a.split_units);
+  const float2* ml = (const float2*)a.part_ml + (size_t)row * a.n_split;
+  const float* part = a.part + (size_t)row * a.n_split * d + col;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (J == 1) {
+    constexpr int kMost = 8;
+    float2 e[kMost];
+    f32x4_t w[kMost];
+#pragma unroll
+    for (int s = 0; s < kMost; ++s) {
+      e[s] = ml[min(s, n - 1)];
+      w[s] = *(const f32x4_t*)(part + (size_t)min(s, n - 1) * d);
+      m = fmaxf(m, e[s].x);
+    }
+#pragma unroll
+    for (int s = 0; s < kMost; ++s) {
+      const float f = (s < n) & (e[s].x != -INFINITY) ? __builtin_amdgcn_exp2f(e[s].x - m) : 0.f;
+      l += f * e[s].y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += f == 0.f ? 0.f : f * w[s][k];
+    }
+  } else {
+#pragma unroll 4
+    for (int s = i; s < n; s += J) m = fmaxf(m, ml[s].x);
+    s_l[i][tid % kCols] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < J; ++k) m = fmaxf(m, s_l[k][tid % kCols]);
+    __syncthreads();
+#pragma unroll 4
+    for (int s = i; s < n; s += J) {
+      const float2 e = ml[s];
+      const float f = e.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e.x - m);
+      l += f * e.y;
+      v += f * *(const f32x4_t*)(part + (size_t)s * d);
+    }
+    s_l[i][tid % kCols] = l;
+    s_v[i][tid % kCols] = v;
+    __syncthreads();
+    if (i > 0) return;
+#pragma unroll
+    for (int k = 1; k < J; ++k) {
+      l += s_l[k][tid];
+      v += s_v[k][tid];
+    }
+  }
+  if (!real) return;
+  if (l != 0.f) v *= 1.f / l;
+  *(f32x4_t*)(a.out + (size_t)row * d + col) = v;
+  if (col == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 }  // namespace sv

@@ -25,9 +25,12 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   return SV_OK;
 }
 
-// How a call is split over the chip: kTargetGroups workgroups where the cache is long enough for that, each at
-// least kMinUnits units of 16 rows.  Splits (and with them the scratch) never get fewer as max_len grows.
-constexpr int kTargetGroups = 1024, kMinUnits = 16;
+// How a call is split over the chip.  768 workgroups run at a time (three per CU); a single sequence is cut into as
+// many pieces, several into four times as many, since some of them are shorter.  A piece has 16 units of 16 rows at
+// least, and one for each query head of a KV head, beside whose rows its results would not be little.
+// Splits (and with them the scratch) never get fewer as max_len grows.
+constexpr int kGroupsOne = 768, kGroupsRagged = 3072, kMinUnits = 16;
+constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
   int n_blocks, n_split, split_units;
   size_t rows, part, part_ml, bytes;
@@ -36,15 +39,24 @@ static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
   PagedPlan p;
   p.n_blocks = ceil_div(n_q / c.n_kv_heads, 16);
   const long long tasks = (long long)c.n_seqs * c.n_kv_heads * p.n_blocks;
-  const int most = (int)(tasks >= kTargetGroups ? 1 : (kTargetGroups + tasks - 1) / tasks);
-  const int fill = n_units / kMinUnits;
+  const long long target = c.n_seqs > 1 ? kGroupsRagged : kGroupsOne;
+  const int most = (int)(tasks >= target ? 1 : (target + tasks - 1) / tasks);
+  const int fill = n_units / (n_q / c.n_kv_heads > kMinUnits ? n_q / c.n_kv_heads : kMinUnits);
+  const int least = ceil_div(n_units, kPagedWaves * kBatchUnits);
   p.n_split = fill < 1 ? 1 : (fill < most ? fill : most);
+  if (p.n_split < least) p.n_split = least;
   p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
   p.rows = (size_t)c.n_seqs * n_q;
   p.part = 0;
   p.part_ml = p.n_split > 1 ? align_up(p.rows * p.n_split * c.head_dim * 4, kAlign) : 0;
   p.bytes = p.n_split > 1 ? p.part_ml + align_up(p.rows * p.n_split * 8, kAlign) : kAlign;
   return p;
+}
+
+// Rows that are read once and fill the Infinity Cache (256 MB) go past the caches.
+static bool past_caches(const sv_paged_cache& c, const PagedPlan& p, int n_units) {
+  const long long row = 2ll * c.n_kv_heads * c.head_dim * (c.dtype == SV_F32 ? 4 : 2);
+  return p.n_blocks == 1 && c.n_seqs * (n_units * 16ll) * row > kInfinityCache;
 }
 
 // Units that the visible rows of any sequence of up to max_len rows lie in, at most.
@@ -103,23 +115,34 @@ int sv_paged_attention(const sv_paged_cache* cache, const int32_t* seq_len, int 
   if (!seq_len || !q || !out || !workspace) return SV_ERR_NULL;
   if (window < 0 || n_sink < 0 || !std::isfinite(scale) || (uintptr_t)q % 16 || (uintptr_t)out % 16) return SV_ERR_SHAPE;
   if ((uintptr_t)workspace % kAlign || ws_bytes < need) return SV_ERR_WORKSPACE;
-  const PagedPlan p = plan_paged(*cache, n_q_heads, most_units(max_len, window, n_sink));
+  const int units = most_units(max_len, window, n_sink);
+  const PagedPlan p = plan_paged(*cache, n_q_heads, units);
   PagedAttnArgs a;
   a.c = view(*cache); a.seq_len = seq_len; a.max_len = max_len; a.n_q = n_q_heads; a.window = window; a.n_sink = n_sink;
   a.n_blocks = p.n_blocks; a.n_split = p.n_split; a.split_units = p.split_units;
   a.scale = scale * 1.4426950408889634f; a.q = q; a.out = out; a.lse = lse; a.status = status;
   a.part = (float*)((char*)workspace + p.part); a.part_ml = (float*)((char*)workspace + p.part_ml);
   hipStream_t st = (hipStream_t)stream;
-  const unsigned groups = (unsigned)((size_t)cache->n_seqs * cache->n_kv_heads * p.n_blocks * p.n_split);
-  auto run = [&](auto t) {
+  const unsigned groups = (unsigned)(((size_t)cache->n_seqs * cache->n_kv_heads * p.n_split + 7) / 8 * 8 * p.n_blocks);
+  auto run = [&](auto t, auto past) {
     using T = decltype(t);
-    if (cache->head_dim <= 64) paged_attention_mfma<T, 64><<<groups, 256, 0, st>>>(a);
-    else if (cache->head_dim <= 128) paged_attention_mfma<T, 128><<<groups, 256, 0, st>>>(a);
-    else paged_attention_mfma<T, 256><<<groups, 256, 0, st>>>(a);
+    constexpr int NT = decltype(past)::value;
+    if (cache->head_dim <= 64) paged_attention_mfma<T, 64, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
+    else if (cache->head_dim <= 128) paged_attention_mfma<T, 128, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
+    else paged_attention_mfma<T, 256, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
   };
-  if (cache->dtype == SV_F32) run(0.f);
-  else run(bf16_t{});
-  if (p.n_split > 1) paged_attention_join<<<dim3(n_q_heads, cache->n_seqs), 256, 0, st>>>(a);
+  auto typed = [&](auto past) {
+    if (cache->dtype == SV_F32) run(0.f, past);
+    else run(bf16_t{}, past);
+  };
+  if (past_caches(*cache, p, units)) typed(std::integral_constant<int, 1>{});
+  else typed(std::integral_constant<int, 0>{});
+  if (p.n_split > 1) {
+    const int joiners = p.n_split <= 8 ? 1 : 32;
+    const unsigned n_join = (unsigned)((p.rows * (cache->head_dim / 4) * joiners + 255) / 256);
+    auto join = joiners == 1 ? paged_attention_join<1> : paged_attention_join<32>;
+    join<<<n_join + (status ? cache->n_seqs : 0), 256, 0, st>>>(a, n_join);
+  }
   return launch_status();
 }
 

@@ -2,6 +2,8 @@
 #ifndef SV_SAMPLE_H
 #define SV_SAMPLE_H
 
+#include <type_traits>
+
 #include "sv_frag.h"
 
 namespace sv {
@@ -24,33 +26,77 @@ __device__ inline float block_reduce(float v, bool maximum, float* red) {
   return v;
 }
 
-// grid = rows, block = NT: maximum, sum, quotients, a pass over the row each.
-template <int NT>
+// grid = rows, block = NT.  A row of up to NT * K columns stays in registers, K of them per thread, and is read once;
+// a longer one (K = 0) is read twice, first for a running maximum and the sum that goes with it.
+template <int NT, int K>
 __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, float inv_t, float* p) {
   __shared__ float red[NT / 64];
   const float* src = z + (size_t)blockIdx.x * n;
   float* dst = p + (size_t)blockIdx.x * n;
-  float m = -INFINITY;
+  float m = -INFINITY, s = 0.f;
   bool nan = false;
-  for (int i = threadIdx.x; i < n; i += NT) {
-    const float v = src[i];
-    nan |= v != v;
-    m = fmaxf(m, v);
+  if constexpr (K > 0) {
+    float v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = src[min(k * NT + (int)threadIdx.x, n - 1)];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      nan |= v[k] != v[k];
+      m = fmaxf(m, v[k]);
+    }
+    m = block_reduce<NT>(m, true, red);
+    if (m == -INFINITY) m = 0.f;             // nothing but -infinity: every term is zero
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = expf((v[k] - m) * inv_t);
+      s += k * NT + (int)threadIdx.x < n ? v[k] : 0.f;
+    }
+    s = block_reduce<NT>(nan ? NAN : s, false, red);
+    const float r = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (k * NT + (int)threadIdx.x < n) dst[k * NT + threadIdx.x] = v[k] * r;
+  } else {
+    constexpr int kBatch = 16;
+    float mine = -INFINITY;
+    for (int i0 = 0; i0 < n; i0 += kBatch * NT) {
+      float v[kBatch], top = mine;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) v[k] = src[min(i0 + k * NT + (int)threadIdx.x, n - 1)];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        nan |= v[k] != v[k];
+        top = fmaxf(top, v[k]);
+      }
+      const float use = top == -INFINITY ? 0.f : top;
+      s *= expf((mine - use) * inv_t);
+      mine = top;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) s += i0 + k * NT + (int)threadIdx.x < n ? expf((v[k] - use) * inv_t) : 0.f;
+    }
+    m = block_reduce<NT>(mine, true, red);
+    if (m == -INFINITY) m = 0.f;
+    s = block_reduce<NT>(nan ? NAN : s * expf((mine - m) * inv_t), false, red);
+    const float r = s == 0.f ? 0.f : 1.f / s;
+    for (int i0 = 0; i0 < n; i0 += kBatch * NT) {
+      float v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) v[k] = src[min(i0 + k * NT + (int)threadIdx.x, n - 1)];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = i0 + k * NT + (int)threadIdx.x;
+        if (i < n) dst[i] = expf((v[k] - m) * inv_t) * r;
+      }
+    }
   }
-  m = block_reduce<NT>(m, true, red);
-  if (m == -INFINITY) m = 0.f;               // nothing but -infinity: every term is zero
-  float s = 0.f;
-  for (int i = threadIdx.x; i < n; i += NT) s += expf((src[i] - m) * inv_t);
-  s = block_reduce<NT>(nan ? NAN : s, false, red);
-  const float r = s == 0.f ? 0.f : 1.f / s;
-  for (int i = threadIdx.x; i < n; i += NT) dst[i] = expf((src[i] - m) * inv_t) * r;
 }
 
 // ---- sampled acceptance ------------------------------------------------------------------------
 // One workgroup walks down one tree.  What the tests need of the nodes - parent, token, p and q of the
-// token in the parent's row, random number - is fetched for all nodes at once; the walk itself is
-// scalar work on LDS values that every wave repeats for itself, so that its branches are uniform over the
-// workgroup.  Only sums over whole rows (a second sibling, the final draw) read the rows.
+// token in the parent's row, random number - is fetched for all nodes at once; each wave then has all nodes in its
+// registers, two a lane, and goes through the walk for itself: children are found by ballot, a child's numbers come
+// by readlane, and the branches are uniform over the workgroup.  Only sums over whole rows (before a second
+// sibling, and for the draw) read the rows.
 // Sums are float64: the inputs are float32, so that a sum is exact unless its terms span more
 // than 2^29, and the choice of a token does not hang on the order of the summation.
 
@@ -70,36 +116,48 @@ __device__ inline double wave_sum_f64(double v) {
   return v;
 }
 
-__device__ inline float mass_of(float p) { return p > 0.f ? p : 0.f; }       // (a NaN has none)
+__device__ inline float mass_of(float p) { return fmaxf(p, 0.f); }       // (a NaN has none)
 
-// What is left of a row: the part of column i that a draw can still hit.
+// What is left of a row: max(p - less q, 0), or p without the refused columns.
+template <bool kDrawn>
 struct RestOfRow {
-  const float *p, *q;        // q: NULL where the children were chosen
+  const float *p, *q;
   double less;
-  const int* refused;        // LDS: columns that do not count
+  const int* refused;        // LDS
   int n_refused;
-  __device__ double at(int i) const {
-    const double v = (double)p[i] - (q ? less * (double)mass_of(q[i]) : 0.0);
-    if (!(v > 0.0)) return 0.0;                    // (a NaN too)
-    for (int r = 0; r < n_refused; ++r)
-      if (refused[r] == i) return 0.0;
-    return v;
+  __device__ double left(float pi, float qi, int i) const {
+    if constexpr (kDrawn) return fmax(fma(-less, (double)mass_of(qi), (double)pi), 0.0);
+    float v = mass_of(pi);
+    for (int r = 0; r < n_refused; ++r) v = refused[r] == i ? 0.f : v;
+    return (double)v;
   }
+  __device__ double at(int i) const { return left(p[i], kDrawn ? q[i] : 0.f, i); }
 };
 
 // Sums over a row, and the column that a cumulated sum of `goal` falls on.  The columns are cut into one run
 // per wave; the run that holds the goal is cut again, until a thread has kLeaf columns.
-template <int NT>
+template <int NT, bool kDrawn>
 struct RowSearch {
-  static constexpr int kWaves = NT / 64, kLeaf = 4;
+  static constexpr int kWaves = NT / 64, kLeaf = 4, kBatch = kDrawn ? 8 : 16;
+  typedef RestOfRow<kDrawn> Row;
   double part[kWaves];       // LDS: sums of the runs
   int hit, last;
 
-  __device__ void sums(const RestOfRow& row, int begin, int end, int run) {
+  __device__ void sums(const Row& row, int begin, int end, int run) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int first = begin + wave * run, stop = min(end, first + run);
     double s = 0.0;
-    for (int i = first + lane; i < stop; i += 64) s += row.at(i);
+    for (int i0 = first + lane; i0 < stop; i0 += 64 * kBatch) {
+      float p[kBatch], q[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = min(i0 + 64 * k, stop - 1);
+        p[k] = row.p[i];
+        q[k] = kDrawn ? row.q[i] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) s += i0 + 64 * k < stop ? row.left(p[k], q[k], i0 + 64 * k) : 0.0;
+    }
     s = wave_sum_f64(s);
     __syncthreads();
     if (lane == 0) part[wave] = s;
@@ -107,29 +165,31 @@ struct RowSearch {
   }
   __device__ static int run_of(int n) { return (n + kWaves - 1) / kWaves; }
   // (leaves the runs' sums in part)
-  __device__ double total(const RestOfRow& row, int n) {
+  __device__ double total(const Row& row, int n) {
     sums(row, 0, n, run_of(n));
     double s = 0.0;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) s += part[w];
     return s;
   }
   // First column with mass at which the cumulated sum exceeds goal, the last one with mass if there is
   // none.  After total(row, n).
-  __device__ int find(const RestOfRow& row, int n, double goal) {
+  __device__ int find(const Row& row, int n, double goal) {
     int begin = 0, end = n;
     double before = 0.0;
     while (end - begin > NT * kLeaf) {
       const int run = run_of(end - begin);
       if (end - begin < n) sums(row, begin, end, run);
       int in = 0;
+      bool found = false;
       double cum = before, at = before;
+#pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        if (part[w] > 0.0) {
-          in = w;
-          at = cum;
-          if (cum + part[w] > goal) break;
-        }
+        const bool here = (part[w] > 0.0) & !found;
+        in = here ? w : in;
+        at = here ? cum : at;
         cum += part[w];
+        found = found | (here & (cum > goal));
       }
       before = at;
       begin += in * run;
@@ -138,8 +198,10 @@ struct RowSearch {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = begin + kLeaf * (int)threadIdx.x;
     double v[kLeaf], mine = 0.0;
 #pragma unroll
+    for (int k = 0; k < kLeaf; ++k) v[k] = row.at(min(first + k, end - 1));
+#pragma unroll
     for (int k = 0; k < kLeaf; ++k) {
-      v[k] = first + k < end ? row.at(first + k) : 0.0;
+      v[k] = first + k < end ? v[k] : 0.0;
       mine += v[k];
     }
     double upto = mine;
@@ -157,110 +219,148 @@ struct RowSearch {
     __syncthreads();
     double cum = before + (upto - mine);
     for (int w = 0; w < wave; ++w) cum += part[w];
+    int my_hit = n, my_last = -1;
+#pragma unroll
+    for (int k = kLeaf - 1; k >= 0; --k)
+      if (v[k] > 0.0 && my_last < 0) my_last = first + k;
 #pragma unroll
     for (int k = 0; k < kLeaf; ++k) {
-      if (!(v[k] > 0.0)) continue;
       cum += v[k];
-      if (cum > goal) atomicMin(&hit, first + k);
-      atomicMax(&last, first + k);
+      if (v[k] > 0.0 && cum > goal && my_hit == n) my_hit = first + k;
     }
+    if (my_hit < n) atomicMin(&hit, my_hit);
+    if (my_last >= 0) atomicMax(&last, my_last);
     __syncthreads();
     return hit < n ? hit : last;
   }
 };
 
-template <int NT>
+// A number per node, two nodes a lane.
+template <typename V>
+struct Nodes {
+  V lo, hi;
+  __device__ Nodes(const V* of_all, int lane) : lo(of_all[lane]), hi(of_all[64 + lane]) {}
+  __device__ V of(int c) const { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c < 64 ? lo : hi), c & 63)); }
+};
+struct NodeSet {
+  unsigned long long lo, hi;
+  __device__ bool has(int c) const { return (c < 64 ? lo : hi) >> (c & 63) & 1; }
+  __device__ void add(int c) {
+    const unsigned long long bit = 1ull << (c & 63);
+    lo |= c < 64 ? bit : 0;
+    hi |= c < 64 ? 0 : bit;
+  }
+  __device__ int take_first() {
+    const bool low = lo != 0;
+    const int c = low ? __builtin_ctzll(lo) : 64 + __builtin_ctzll(hi);
+    hi = low ? hi : hi & (hi - 1);
+    lo &= lo - 1;            // (0 stays 0)
+    return c;
+  }
+};
+
+template <int NT, bool kDrawn>
 __global__ __launch_bounds__(NT) void sampled_accept_kernel(const SampleArgs a) {
-  __shared__ RowSearch<NT> search;
+  __shared__ RowSearch<NT, kDrawn> search;
   __shared__ int s_parent[SV_MAX_TREE_NODES], s_col[SV_MAX_TREE_NODES], s_refused[SV_MAX_TREE_NODES];
   __shared__ float s_p[SV_MAX_TREE_NODES], s_q[SV_MAX_TREE_NODES], s_u[SV_MAX_TREE_NODES];
-  const int b = blockIdx.x, tid = threadIdx.x, T = a.T, n = a.n_vocab;
+  __shared__ int s_path[SV_MAX_DEPTH + 1];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, T = a.T, n = a.n_vocab;
   const size_t base = (size_t)b * T;
-  int32_t* path = a.path + (size_t)b * (a.d_cap + 1);
-  int32_t* out = a.out_tokens + (size_t)b * (a.d_cap + 1);
-  for (int c = tid; c < T; c += NT) {
-    int par = c ? a.parent[base + c] : -1;
-    if (par >= c) par = -1;
-    const long long col = (long long)a.token[base + c] - a.lo;
-    const bool in = par >= 0 && col >= 0 && col < n;
-    s_parent[c] = par;
-    s_col[c] = in ? (int)col : -1;
-    s_u[c] = a.u_accept[base + c];
-    s_p[c] = in ? mass_of(a.target[(base + par) * n + col]) : 0.f;
-    s_q[c] = in && a.draft ? mass_of(a.draft[(base + par) * n + col]) : 0.f;
-    a.accept_mask[base + c] = c == 0;
-  }
-  for (int i = tid; i <= a.d_cap; i += NT) {
-    path[i] = i ? -1 : 0;
-    out[i] = -1;
-  }
-  __syncthreads();
-
-  int node = 0, depth = 0, n_refused = 0;
-  double less = 0.0, mass = 1.0;
-  bool stale = false;                        // mass is that of before the last refusal
-  RestOfRow row{a.target + base * n, a.draft ? a.draft + base * n : nullptr, 0.0, s_refused, 0};
-  if (depth < a.d_cap)
-    for (int c = 1; c < T; ++c) {
-      if (s_parent[c] != node) continue;
-      const int x = s_col[c];
-      double p = s_p[c];
-      bool take;
-      if (a.draft) {
-        if (stale) mass = search.total(row, n);
-        stale = false;
-        double left = p - less * (double)s_q[c];
-        left = left > 0.0 ? left : 0.0;
-        take = (double)s_u[c] * (double)s_q[c] * mass < left;
-        if (!take) {
-          less += mass;
-          stale = true;
-          row.less = less;
-        }
-      } else {
-        for (int r = 0; r < n_refused; ++r)
-          if (s_refused[r] == x) p = 0.0;
-        take = (double)s_u[c] * mass < p;
-        if (!take) {
-          if (p > 0.0) mass = mass > p ? mass - p : 0.0;
-          __syncthreads();
-          if (tid == 0) s_refused[n_refused] = x;
-          __syncthreads();
-          ++n_refused;
-        }
-      }
-      if (!take) continue;
-      node = c;
-      ++depth;
-      less = 0.0; mass = 1.0; stale = false; n_refused = 0;
-      row.p = a.target + (base + c) * n;
-      row.q = a.draft ? a.draft + (base + c) * n : nullptr;
-      row.less = 0.0;
-      if (tid == 0) {
-        a.accept_mask[base + c] = 1;
-        path[depth] = c;
-        out[depth - 1] = x + a.lo;
-      }
-      if (depth >= a.d_cap) break;
+  for (int c = tid; c < SV_MAX_TREE_NODES; c += NT) {
+    int par = -1;
+    if (c > 0 && c < T) {
+      par = a.parent[base + c];
+      const long long col = (long long)a.token[base + c] - a.lo;
+      s_u[c] = a.u_accept[base + c];
+      if (par >= c) par = -1;
+      const bool in = par >= 0 && col >= 0 && col < n;
+      s_col[c] = in ? (int)col : -1;
+      s_p[c] = in ? mass_of(a.target[(base + par) * n + col]) : 0.f;
+      s_q[c] = in && kDrawn ? mass_of(a.draft[(base + par) * n + col]) : 0.f;
     }
+    s_parent[c] = par;
+  }
+  const double u_draw = a.u_draw[b];
   __syncthreads();
+  const Nodes<int> par(s_parent, lane), cols(s_col, lane);
+  const Nodes<float> ps(s_p, lane), qs(s_q, lane), us(s_u, lane);
 
-  // the draw
-  row.n_refused = n_refused;
+  int node = 0, depth = 0;
+  NodeSet taken{1, 0}, kids;
+  double less = 0.0;
+  RestOfRow<kDrawn> row{a.target + base * n, kDrawn ? a.draft + base * n : nullptr, 0.0, s_refused, 0};
+  for (;;) {
+    kids = NodeSet{0, 0};
+    if (depth < a.d_cap) kids = NodeSet{__builtin_amdgcn_ballot_w64(par.lo == node), __builtin_amdgcn_ballot_w64(par.hi == node)};
+    NodeSet todo = kids;
+    int next = -1;
+    double mass = 1.0;
+    bool stale = false;                      // mass is that of before the last refusal
+    less = 0.0;
+    while (todo.lo | todo.hi) {
+      const int c = todo.take_first();
+      double p = ps.of(c);
+      const double u = us.of(c);
+      bool take;
+      if constexpr (kDrawn) {
+        if (stale) {
+          row.less = less;
+          mass = search.total(row, n);
+        }
+        const double q = qs.of(c), rest = fmax(fma(-less, q, p), 0.0);
+        take = u * q * mass < rest;
+        less += take ? 0.0 : mass;
+        stale = true;
+      } else {
+        const int x = cols.of(c);
+        // an earlier sibling of the same token has been refused
+        if (__builtin_amdgcn_ballot_w64((par.lo == node && cols.lo == x && lane < c) || (par.hi == node && cols.hi == x && 64 + lane < c))) p = 0.0;
+        take = u * mass < p;
+        if (!take) mass = mass > p ? mass - p : 0.0;
+      }
+      if (take) {
+        next = c;
+        break;
+      }
+    }
+    if (next < 0) break;
+    node = next;
+    ++depth;
+    taken.add(node);
+    if (tid == 0) s_path[depth] = node;
+    row.p = a.target + (base + node) * n;
+    if (kDrawn) row.q = a.draft + (base + node) * n;
+  }
+
+  // the draw: from what the refused children (all of the last node's) have left
+  row.less = less;
+  if constexpr (!kDrawn) {
+    const unsigned long long before = (1ull << lane) - 1;
+    if (tid < 64 && kids.lo >> lane & 1) s_refused[__builtin_popcountll(kids.lo & before)] = cols.lo;
+    if (tid < 64 && kids.hi >> lane & 1) s_refused[__builtin_popcountll(kids.lo) + __builtin_popcountll(kids.hi & before)] = cols.hi;
+    row.n_refused = __builtin_popcountll(kids.lo) + __builtin_popcountll(kids.hi);
+  }
+  __syncthreads();
   double w = search.total(row, n);
   int status = 0;
   if (!(w > 0.0)) {
     status = 1;
-    row.q = nullptr;
+    row.less = 0.0;
     row.n_refused = 0;
     w = search.total(row, n);
     if (!(w > 0.0)) status = 3;
   }
-  const int col = search.find(row, n, (double)a.u_draw[b] * w);
+  const int col = search.find(row, n, u_draw * w);
+  for (int c = tid; c < T; c += NT) a.accept_mask[base + c] = taken.has(c);
+  if (tid <= a.d_cap) {
+    const size_t at = (size_t)b * (a.d_cap + 1) + tid;
+    a.path[at] = tid == 0 ? 0 : (tid <= depth ? s_path[tid] : -1);
+    a.out_tokens[at] = tid < depth ? s_col[s_path[tid + 1]] + a.lo : (tid > depth ? -1 : a.lo + (status == 3 ? 0 : col));
+  }
   if (tid == 0) {
     a.accepted_len[b] = depth;
     a.best_node[b] = node;
-    out[depth] = a.lo + (status == 3 ? 0 : col);
     a.status[b] = status;
   }
 }

@@ -10,14 +10,23 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
   if (n_rows < 1 || n_rows >= (1 << 21) || n_vocab < 1 || n_vocab > SV_MAX_SAMPLED_VOCAB) return SV_ERR_SHAPE;
   const float inv_t = 1.f / temperature;
   if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t)) return SV_ERR_TOKEN;
-  if (n_vocab > 2048) token_probs_kernel<1024><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
-  else token_probs_kernel<64><<<n_rows, 64, 0, st>>>(logits, n_vocab, inv_t, probs);
+  if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, inv_t, probs);
+  else if (n_vocab <= 2048) token_probs_kernel<256, 8><<<n_rows, 256, 0, st>>>(logits, n_vocab, inv_t, probs);
+  else if (n_vocab <= 8192) token_probs_kernel<1024, 8><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
+  else if (n_vocab <= 32768) token_probs_kernel<1024, 32><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
+  else token_probs_kernel<1024, 0><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
   return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH;
 }
 
 static int sampled_accept(const SampleArgs& a, int B, hipStream_t st) {
-  if (a.n_vocab > 2048) sampled_accept_kernel<1024><<<B, 1024, 0, st>>>(a);
-  else sampled_accept_kernel<256><<<B, 256, 0, st>>>(a);
+  auto run = [&](auto drawn) {
+    constexpr bool kDrawn = decltype(drawn)::value;
+    if (a.n_vocab <= 256) sampled_accept_kernel<64, kDrawn><<<B, 64, 0, st>>>(a);
+    else if (a.n_vocab <= 2048) sampled_accept_kernel<256, kDrawn><<<B, 256, 0, st>>>(a);
+    else sampled_accept_kernel<1024, kDrawn><<<B, 1024, 0, st>>>(a);
+  };
+  if (a.draft) run(std::true_type{});
+  else run(std::false_type{});
   return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH;
 }
 

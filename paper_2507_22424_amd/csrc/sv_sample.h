@@ -10,6 +10,8 @@ namespace sv {
 
 // ---- probabilities from logits -----------------------------------------------------------------
 
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
 template <int NT>
 __device__ inline float block_reduce(float v, bool maximum, float* red) {
 #pragma unroll
@@ -29,7 +31,7 @@ __device__ inline float block_reduce(float v, bool maximum, float* red) {
 // grid = rows, block = NT.  A row of up to NT * K columns stays in registers, K of them per thread, and is read once;
 // a longer one (K = 0) is read twice, first for a running maximum and the sum that goes with it.
 template <int NT, int K>
-__global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, float inv_t, float* p) {
+__global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, float c, float* p) {
   __shared__ float red[NT / 64];
   const float* src = z + (size_t)blockIdx.x * n;
   float* dst = p + (size_t)blockIdx.x * n;
@@ -48,7 +50,7 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
     if (m == -INFINITY) m = 0.f;             // nothing but -infinity: every term is zero
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      v[k] = expf((v[k] - m) * inv_t);
+      v[k] = exp2_of((v[k] - m) * c);
       s += k * NT + (int)threadIdx.x < n ? v[k] : 0.f;
     }
     s = block_reduce<NT>(nan ? NAN : s, false, red);
@@ -69,14 +71,14 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
         top = fmaxf(top, v[k]);
       }
       const float use = top == -INFINITY ? 0.f : top;
-      s *= expf((mine - use) * inv_t);
+      s *= exp2_of((mine - use) * c);
       mine = top;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) s += i0 + k * NT + (int)threadIdx.x < n ? expf((v[k] - use) * inv_t) : 0.f;
+      for (int k = 0; k < kBatch; ++k) s += i0 + k * NT + (int)threadIdx.x < n ? exp2_of((v[k] - use) * c) : 0.f;
     }
     m = block_reduce<NT>(mine, true, red);
     if (m == -INFINITY) m = 0.f;
-    s = block_reduce<NT>(nan ? NAN : s * expf((mine - m) * inv_t), false, red);
+    s = block_reduce<NT>(nan ? NAN : s * exp2_of((mine - m) * c), false, red);
     const float r = s == 0.f ? 0.f : 1.f / s;
     for (int i0 = 0; i0 < n; i0 += kBatch * NT) {
       float v[kBatch];
@@ -85,7 +87,7 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const int i = i0 + k * NT + (int)threadIdx.x;
-        if (i < n) dst[i] = expf((v[k] - m) * inv_t) * r;
+        if (i < n) dst[i] = exp2_of((v[k] - m) * c) * r;
       }
     }
   }
@@ -119,53 +121,71 @@ __device__ inline double wave_sum_f64(double v) {
 __device__ inline float mass_of(float p) { return fmaxf(p, 0.f); }       // (a NaN has none)
 
 // What is left of a row: max(p - less q, 0), or p without the refused columns.
-template <bool kDrawn>
 struct RestOfRow {
   const float *p, *q;
-  double less;
+  double less;               // 0: q is not read
   const int* refused;        // LDS
   int n_refused;
-  __device__ double left(float pi, float qi, int i) const {
-    if constexpr (kDrawn) return fmax(fma(-less, (double)mass_of(qi), (double)pi), 0.0);
-    float v = mass_of(pi);
-    for (int r = 0; r < n_refused; ++r) v = refused[r] == i ? 0.f : v;
-    return (double)v;
-  }
-  __device__ double at(int i) const { return left(p[i], kDrawn ? q[i] : 0.f, i); }
 };
+
+// Of columns i, i + STEP, ..: kFull if all N lie before `end`, else what lies behind counts 0.
+template <int N, int STEP, bool kQ, bool kFull>
+__device__ inline void rest_at(const RestOfRow& row, int i, int end, double* v) {
+  float p[N], q[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int at = kFull ? i + k * STEP : min(i + k * STEP, end - 1);
+    p[k] = row.p[at];
+    q[k] = kQ ? row.q[at] : 0.f;
+  }
+  for (int r = 0; r < row.n_refused; ++r) {
+    const int x = row.refused[r];
+#pragma unroll
+    for (int k = 0; k < N; ++k) p[k] = i + k * STEP == x ? 0.f : p[k];
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = kQ ? fmax(fma(-row.less, (double)mass_of(q[k]), (double)p[k]), 0.0) : (double)mass_of(p[k]);
+    if (!kFull) v[k] = i + k * STEP < end ? v[k] : 0.0;
+  }
+}
 
 // Sums over a row, and the column that a cumulated sum of `goal` falls on.  The columns are cut into one run
 // per wave; the run that holds the goal is cut again, until a thread has kLeaf columns.
-template <int NT, bool kDrawn>
+template <int NT>
 struct RowSearch {
-  static constexpr int kWaves = NT / 64, kLeaf = 4, kBatch = kDrawn ? 8 : 16;
-  typedef RestOfRow<kDrawn> Row;
+  static constexpr int kWaves = NT / 64, kLeaf = 4, kBatch = NT == 64 ? 4 : 8;
   double part[kWaves];       // LDS: sums of the runs
   int hit, last;
 
-  __device__ void sums(const Row& row, int begin, int end, int run) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int first = begin + wave * run, stop = min(end, first + run);
-    double s = 0.0;
-    for (int i0 = first + lane; i0 < stop; i0 += 64 * kBatch) {
-      float p[kBatch], q[kBatch];
+  template <bool kQ>
+  __device__ static double lane_sum(const RestOfRow& row, int first, int stop) {
+    const int lane = threadIdx.x & 63;
+    double s = 0.0, v[kBatch];
+    int i = first;
+    for (; i + 64 * kBatch <= stop; i += 64 * kBatch) {
+      rest_at<kBatch, 64, kQ, true>(row, i + lane, stop, v);
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int i = min(i0 + 64 * k, stop - 1);
-        p[k] = row.p[i];
-        q[k] = kDrawn ? row.q[i] : 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) s += i0 + 64 * k < stop ? row.left(p[k], q[k], i0 + 64 * k) : 0.0;
+      for (int k = 0; k < kBatch; ++k) s += v[k];
     }
-    s = wave_sum_f64(s);
+    if (i < stop) {
+      rest_at<kBatch, 64, kQ, false>(row, i + lane, stop, v);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) s += v[k];
+    }
+    return s;
+  }
+  __device__ void sums(const RestOfRow& row, int begin, int end, int run) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int first = begin + wave * run, stop = min(end, first + run);
+    const double s = wave_sum_f64(row.less != 0.0 ? lane_sum<true>(row, first, stop) : lane_sum<false>(row, first, stop));
     __syncthreads();
-    if (lane == 0) part[wave] = s;
+    if ((threadIdx.x & 63) == 0) part[wave] = s;
     __syncthreads();
   }
   __device__ static int run_of(int n) { return (n + kWaves - 1) / kWaves; }
   // (leaves the runs' sums in part)
-  __device__ double total(const Row& row, int n) {
+  __device__ double total(const RestOfRow& row, int n) {
     sums(row, 0, n, run_of(n));
     double s = 0.0;
 #pragma unroll
@@ -174,7 +194,7 @@ struct RowSearch {
   }
   // First column with mass at which the cumulated sum exceeds goal, the last one with mass if there is
   // none.  After total(row, n).
-  __device__ int find(const Row& row, int n, double goal) {
+  __device__ int find(const RestOfRow& row, int n, double goal) {
     int begin = 0, end = n;
     double before = 0.0;
     while (end - begin > NT * kLeaf) {
@@ -197,13 +217,10 @@ struct RowSearch {
     }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = begin + kLeaf * (int)threadIdx.x;
     double v[kLeaf], mine = 0.0;
+    if (row.less != 0.0) rest_at<kLeaf, 1, true, false>(row, first, end, v);
+    else rest_at<kLeaf, 1, false, false>(row, first, end, v);
 #pragma unroll
-    for (int k = 0; k < kLeaf; ++k) v[k] = row.at(min(first + k, end - 1));
-#pragma unroll
-    for (int k = 0; k < kLeaf; ++k) {
-      v[k] = first + k < end ? v[k] : 0.0;
-      mine += v[k];
-    }
+    for (int k = 0; k < kLeaf; ++k) mine += v[k];
     double upto = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -261,7 +278,7 @@ struct NodeSet {
 
 template <int NT, bool kDrawn>
 __global__ __launch_bounds__(NT) void sampled_accept_kernel(const SampleArgs a) {
-  __shared__ RowSearch<NT, kDrawn> search;
+  __shared__ RowSearch<NT> search;
   __shared__ int s_parent[SV_MAX_TREE_NODES], s_col[SV_MAX_TREE_NODES], s_refused[SV_MAX_TREE_NODES];
   __shared__ float s_p[SV_MAX_TREE_NODES], s_q[SV_MAX_TREE_NODES], s_u[SV_MAX_TREE_NODES];
   __shared__ int s_path[SV_MAX_DEPTH + 1];
@@ -289,7 +306,7 @@ __global__ __launch_bounds__(NT) void sampled_accept_kernel(const SampleArgs a) 
   int node = 0, depth = 0;
   NodeSet taken{1, 0}, kids;
   double less = 0.0;
-  RestOfRow<kDrawn> row{a.target + base * n, kDrawn ? a.draft + base * n : nullptr, 0.0, s_refused, 0};
+  RestOfRow row{a.target + base * n, kDrawn ? a.draft + base * n : nullptr, 0.0, s_refused, 0};
   for (;;) {
     kids = NodeSet{0, 0};
     if (depth < a.d_cap) kids = NodeSet{__builtin_amdgcn_ballot_w64(par.lo == node), __builtin_amdgcn_ballot_w64(par.hi == node)};

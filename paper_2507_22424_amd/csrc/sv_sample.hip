@@ -8,13 +8,13 @@ namespace sv {
 static int token_probs(const float* logits, int n_rows, int n_vocab, float temperature, float* probs, hipStream_t st) {
   if (!logits || !probs) return SV_ERR_NULL;
   if (n_rows < 1 || n_rows >= (1 << 21) || n_vocab < 1 || n_vocab > SV_MAX_SAMPLED_VOCAB) return SV_ERR_SHAPE;
-  const float inv_t = 1.f / temperature;
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t)) return SV_ERR_TOKEN;
-  if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, inv_t, probs);
-  else if (n_vocab <= 2048) token_probs_kernel<256, 8><<<n_rows, 256, 0, st>>>(logits, n_vocab, inv_t, probs);
-  else if (n_vocab <= 8192) token_probs_kernel<1024, 8><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
-  else if (n_vocab <= 32768) token_probs_kernel<1024, 32><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
-  else token_probs_kernel<1024, 0><<<n_rows, 1024, 0, st>>>(logits, n_vocab, inv_t, probs);
+  const float inv_t = 1.f / temperature, c = (float)(1.4426950408889634 / (double)temperature);
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t) || !std::isfinite(c)) return SV_ERR_TOKEN;
+  if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, c, probs);
+  else if (n_vocab <= 2048) token_probs_kernel<256, 8><<<n_rows, 256, 0, st>>>(logits, n_vocab, c, probs);
+  else if (n_vocab <= 8192) token_probs_kernel<1024, 8><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);
+  else if (n_vocab <= 32768) token_probs_kernel<1024, 32><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);
+  else token_probs_kernel<1024, 0><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);
   return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH;
 }
 

@@ -12,8 +12,8 @@ struct PagedCache {
   int n_seqs, max_pages, n_pages, page_size, n_kv, d;
 };
 
-__device__ inline void store_row(float* p, float v) { *p = v; }
-__device__ inline void store_row(bf16_t* p, float v) { p->bits = (uint16_t)pack_bf16x2(v, v); }
+__device__ inline void store4(float* p, f32x4_t v) { *(f32x4_t*)p = v; }
+__device__ inline void store4(bf16_t* p, f32x4_t v) { *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
 
 // ---- append ------------------------------------------------------------------------------------
 
@@ -29,20 +29,26 @@ struct AppendArgs {
 };
 
 // grid = tokens, block = 256.  The rotation's angle is taken in turns and reduced in float64: at position 10^6 a
-// float32 angle is off by 0.06.
+// float32 angle is off by 0.06.  A thread turns four pairs of a head; the values, which need no angle, go first.
 template <typename T>
 __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
-  __shared__ float s_cos[SV_MAX_PAGED_HEAD_DIM / 2], s_sin[SV_MAX_PAGED_HEAD_DIM / 2];
-  const int t = blockIdx.x, tid = threadIdx.x, d = a.c.d, half = d / 2;
-  const int seq = a.seq[t], pos = a.pos[t];
-  int status = seq < 0 ? 1 : (seq >= a.c.n_seqs || pos < 0 || pos / a.c.page_size >= a.c.max_pages ? 2 : 0);
+  __shared__ __attribute__((aligned(16))) float s_cos[SV_MAX_PAGED_HEAD_DIM / 2], s_sin[SV_MAX_PAGED_HEAD_DIM / 2];
+  const int t = blockIdx.x, tid = threadIdx.x, d = a.c.d, half = d / 2, quads = half / 4;
+  const int seq = a.seq[t], pos = a.pos[t], in_seq = pos / a.c.page_size;
+  int status = seq < 0 ? 1 : (seq >= a.c.n_seqs || pos < 0 || in_seq >= a.c.max_pages ? 2 : 0);
   int page = 0;
   if (status == 0) {
-    page = a.c.table[(size_t)seq * a.c.max_pages + pos / a.c.page_size];
+    page = a.c.table[(size_t)seq * a.c.max_pages + in_seq];
     if (page < 0 || page >= a.c.n_pages) status = 4;
   }
   if (a.status && tid == 0) a.status[t] = status;
   if (status) return;
+  const size_t row0 = (size_t)page * a.c.n_kv * a.c.page_size + (pos - in_seq * a.c.page_size);     // of KV head 0
+  const float *q = a.q + t * a.q_stride, *k = a.k + t * a.k_stride, *v = a.v + t * a.v_stride;
+  for (int i = tid; i < a.c.n_kv * 2 * quads; i += 256) {
+    const int h = i / (2 * quads), e = (i - h * 2 * quads) * 4;
+    store4((T*)a.c.v + (row0 + (size_t)h * a.c.page_size) * d + e, *(const f32x4_t*)(v + 4 * i));
+  }
   if (tid < half) {
     const double turns = (double)pos * exp2(-2.0 * tid / d * a.log2_theta) * 0.15915494309189533577;
     const float x = (float)(2.0 * (turns - rint(turns)));
@@ -50,27 +56,22 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
     s_sin[tid] = sinpif(x);
   }
   __syncthreads();
-  const int row = pos % a.c.page_size;
-  const float *q = a.q + t * a.q_stride, *k = a.k + t * a.k_stride, *v = a.v + t * a.v_stride;
-  for (int i = tid; i < (a.n_q + a.c.n_kv) * half; i += 256) {
-    const int h = i / half, e = i - h * half;
+  for (int i = tid; i < (a.n_q + a.c.n_kv) * quads; i += 256) {
+    const int h = i / quads, e = (i - h * quads) * 4;
     const bool is_q = h < a.n_q;
-    const float* src = is_q ? q + h * d : k + (h - a.n_q) * d;
-    const float x = src[e], y = src[e + half], c = s_cos[e], s = s_sin[e];
-    const float x2 = x * c - y * s, y2 = y * c + x * s;
+    const float* src = (is_q ? q + h * d : k + (h - a.n_q) * d) + e;
+    const f32x4_t x = *(const f32x4_t*)src, y = *(const f32x4_t*)(src + half);
+    const f32x4_t c = *(const f32x4_t*)(s_cos + e), s = *(const f32x4_t*)(s_sin + e);
+    const f32x4_t x2 = x * c - y * s, y2 = y * c + x * s;
     if (is_q) {
-      float* dst = a.q_out + ((size_t)t * a.n_q + h) * d;
-      dst[e] = x2;
-      dst[e + half] = y2;
+      float* dst = a.q_out + ((size_t)t * a.n_q + h) * d + e;
+      store4(dst, x2);
+      store4(dst + half, y2);
     } else {
-      T* dst = (T*)a.c.k + (((size_t)page * a.c.n_kv + h - a.n_q) * a.c.page_size + row) * d;
-      store_row(dst + e, x2);
-      store_row(dst + e + half, y2);
+      T* dst = (T*)a.c.k + (row0 + (size_t)(h - a.n_q) * a.c.page_size) * d + e;
+      store4(dst, x2);
+      store4(dst + half, y2);
     }
-  }
-  for (int i = tid; i < a.c.n_kv * d; i += 256) {
-    const int h = i / d, e = i - h * d;
-    store_row((T*)a.c.v + (((size_t)page * a.c.n_kv + h) * a.c.page_size + row) * d + e, v[i]);
   }
 }
 

@@ -25,11 +25,15 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   return SV_OK;
 }
 
-// How a call is split over the chip.  768 workgroups run at a time (three per CU); a single sequence is cut into as
-// many pieces, several into four times as many, since some of them are shorter.  A piece has 16 units of 16 rows at
-// least, and one for each query head of a KV head, beside whose rows its results would not be little.
+// How a call is split over the chip, in workgroups' rounds (a tile for each of the four waves: 128 rows of a bf16
+// cache, 64 of a float32 one).  Up to one workgroup per CU a piece may be as short as a round, if there are three
+// pieces at least (the second launch, which joins them, takes 4 us): 600 tokens, 8 KV heads, 11.4 us in one piece, 9.3 in four.
+// Beyond, a piece has four rounds (32 sequences of up to 1000 tokens: 18.7 us in one piece, 21.3 in three, 24.5 in six),
+// and there are as many as run at a time (three per CU), or four times as many for several sequences, some of which
+// are shorter than others (64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in 3072).  A piece has a unit of 16 rows at least
+// for each query head of a KV head, beside whose rows its results would not be little.
 // Splits (and with them the scratch) never get fewer as max_len grows.
-constexpr int kGroupsOne = 768, kGroupsRagged = 3072, kMinUnits = 16;
+constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 3072;
 constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
   int n_blocks, n_split, split_units;
@@ -38,13 +42,16 @@ struct PagedPlan {
 static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
   PagedPlan p;
   p.n_blocks = ceil_div(n_q / c.n_kv_heads, 16);
-  const long long tasks = (long long)c.n_seqs * c.n_kv_heads * p.n_blocks;
-  const long long target = c.n_seqs > 1 ? kGroupsRagged : kGroupsOne;
-  const int most = (int)(tasks >= target ? 1 : (target + tasks - 1) / tasks);
-  const int fill = n_units / (n_q / c.n_kv_heads > kMinUnits ? n_q / c.n_kv_heads : kMinUnits);
-  const int least = ceil_div(n_units, kPagedWaves * kBatchUnits);
-  p.n_split = fill < 1 ? 1 : (fill < most ? fill : most);
-  if (p.n_split < least) p.n_split = least;
+  const int tasks = c.n_seqs * c.n_kv_heads * p.n_blocks;        // (2^30 at most)
+  const int G = n_q / c.n_kv_heads, round = kPagedWaves * (c.dtype == SV_F32 ? 1 : 2);
+  auto pieces = [&](long long most, int least_units, int least_pieces) {
+    const int fill = n_units / (G > least_units ? G : least_units);
+    return fill < least_pieces ? 1 : (int)(fill < most ? fill : most);
+  };
+  p.n_split = 1;
+  for (const int n : {pieces(kGroupsSmall / tasks, round, 3), pieces(ceil_div(c.n_seqs > 1 ? kGroupsRagged : kGroupsOne, tasks), 4 * round, 2),
+                      ceil_div(n_units, kPagedWaves * kBatchUnits)})
+    p.n_split = n > p.n_split ? n : p.n_split;
   p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
   p.rows = (size_t)c.n_seqs * n_q;
   p.part = 0;

@@ -154,6 +154,34 @@ __device__ inline V load_row(const char* p) {
 
 // A tile of the cache in registers and its two products.  DP: head_dim rounded up to 64, 128 or 256 (columns
 // behind head_dim: q is zero, K and V repeat columns of the row, and the outputs are not stored).
+// The K rows of a tile on their way from the cache to the operand: fetched with the 16 bytes of neighbouring lanes next to
+// each other, and turned by LDS into a row per lane.  (Fetched as operands, 16 neighbouring lanes touch 16 rows, and the
+// cache in front of the L2 looks up 64 lines for an instruction.)  In LDS the 16-byte pieces of row r change places by an
+// exclusive or with r, so that 16 lanes that read the same piece of 16 rows hit different banks.
+template <int kUnits, int kRowBytes, int NT>
+struct PagedKeys {
+  static constexpr int kPieces = kRowBytes / 16, kLoads = kPieces / 4, kMask = (kPieces < 16 ? kPieces : 16) - 1;
+  u32x4_t r[kUnits][kLoads];
+  // row_bytes: of a row in the cache (pieces behind it: its last one again)
+  __device__ void load(int u, const char* base, int row_bytes, int lane) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int i = n * 64 + lane;
+      r[u][n] = load_row<NT, u32x4_t>(base + (unsigned)(i / kPieces * row_bytes + min(i % kPieces * 16, row_bytes - 16)));
+    }
+  }
+  __device__ void stage(u32x4_t* lds, int lane) const {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const int i = n * 64 + lane, row = i / kPieces;
+        lds[u * 16 * kPieces + row * kPieces + ((i % kPieces) ^ (row & kMask))] = r[u][n];
+      }
+  }
+  static __device__ u32x4_t piece(const u32x4_t* lds, int u, int c, int i) { return lds[u * 16 * kPieces + c * kPieces + (i ^ (c & kMask))]; }
+};
+
 template <typename T, int DP, int NT>
 struct PagedTile;
 
@@ -162,7 +190,8 @@ struct PagedTile<bf16_t, DP, NT> {
   static constexpr int kUnits = 2, kSteps = DP / 32, kOut = DP / 16;
   static constexpr int kE = DP / 16 < 8 ? DP / 16 : 8, kLoads = DP / 16 / kE;    // V: elements of a load, loads of a row
   static constexpr int kScores = 8;
-  uint4 k[2][kSteps];
+  typedef PagedKeys<kUnits, DP * 2, NT> Keys;
+  Keys k;
   uint32_t v[8][kE / 2 * kLoads];
   typedef uint4 QPart;
   static constexpr int kParts = 3;           // of the query operand of a step
@@ -173,13 +202,6 @@ struct PagedTile<bf16_t, DP, NT> {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = real && 32 * s + 8 * g < d ? src[32 * s + 8 * g + e] * scale : 0.f;
     split8_3(x, part);
-  }
-  __device__ void load_k(int u, const char* base, int d, int g, int c) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int col = min(32 * s + 8 * g, d - 8);
-      k[u][s] = load_row<NT, uint4>(base + (unsigned)(c * d + col) * 2u);
-    }
   }
   __device__ void load_v(int u, const char* base, int d, int g, int c) {
 #pragma unroll
@@ -201,17 +223,19 @@ struct PagedTile<bf16_t, DP, NT> {
 #pragma unroll
     for (int w = 0; w < kE / 2 * kLoads; ++w) v[e][w] = seen ? v[e][w] : 0;
   }
-  // q: LDS, [part][64 lanes]
-  __device__ void scores(const QPart (*q)[64], int lane, float* x) const {
+  // q, keys: LDS, q as [part][64 lanes]
+  static __device__ void scores(const QPart (*q)[64], const u32x4_t* keys, int lane, int g, int c, float* x) {
     f32x4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int p = 2; p >= 0; --p)
+    for (int i = 0; i < kSteps; ++i) {
+      const uint4 k0 = __builtin_bit_cast(uint4, Keys::piece(keys, 0, c, 4 * i + g)), k1 = __builtin_bit_cast(uint4, Keys::piece(keys, 1, c, 4 * i + g));
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
+      for (int p = 2; p >= 0; --p) {
         const uint4 w = q[3 * i + p][lane];
-        s[0] = mfma_bf16(k[0][i], w, s[0]);
-        s[1] = mfma_bf16(k[1][i], w, s[1]);
+        s[0] = mfma_bf16(k0, w, s[0]);
+        s[1] = mfma_bf16(k1, w, s[1]);
       }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = s[e / 4][e % 4];
   }
@@ -236,7 +260,9 @@ template <int DP, int NT>
 struct PagedTile<float, DP, NT> {
   static constexpr int kUnits = 1, kSteps = DP / 16, kOut = DP / 16;
   static constexpr int kScores = 4;
-  f32x4_t k[1][kSteps], v[4][DP / 64];
+  typedef PagedKeys<kUnits, DP * 4, NT> Keys;
+  Keys k;
+  f32x4_t v[4][DP / 64];
   typedef f32x4_t QPart;
   static constexpr int kParts = 1;
 
@@ -244,10 +270,6 @@ struct PagedTile<float, DP, NT> {
   static __device__ void load_q(int s, const float* src, bool real, float scale, int d, int g, QPart* part) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) part[0][e] = real && 16 * s + 4 * g < d ? src[16 * s + 4 * g + e] * scale : 0.f;
-  }
-  __device__ void load_k(int, const char* base, int d, int g, int c) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[0][s] = load_row<NT, f32x4_t>(base + (unsigned)(c * d + min(16 * s + 4 * g, d - 4)) * 4u);
   }
   __device__ void load_v(int, const char* base, int d, int g, int c) {
 #pragma unroll
@@ -262,13 +284,13 @@ struct PagedTile<float, DP, NT> {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[e][l][i] = seen ? v[e][l][i] : 0.f;
   }
-  __device__ void scores(const QPart (*q)[64], int lane, float* x) const {
+  static __device__ void scores(const QPart (*q)[64], const u32x4_t* keys, int lane, int g, int c, float* x) {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const f32x4_t w = q[i][lane];
+      const f32x4_t k0 = __builtin_bit_cast(f32x4_t, Keys::piece(keys, 0, c, 4 * i + g)), w = q[i][lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], w[e], s, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k0[e], w[e], s, 0, 0, 0);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] = s[r];
@@ -286,24 +308,27 @@ struct PagedTile<float, DP, NT> {
 // kBatchUnits of them per wave.  grid.x = sequences * KV heads * splits, rounded up to a multiple of 8, * blocks.
 constexpr int kBatchUnits = 64, kPagedWaves = 4;
 template <typename T, int DP, int NT>
-__global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_attention_mfma(const PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : (DP == 128 && sizeof(T) == 4 ? 2 : 3)) void paged_attention_mfma(const PagedAttnArgs a) {
   using Tile = PagedTile<T, DP, NT>;
   constexpr int kU = Tile::kUnits, kPitch = DP + 4, NW = kPagedWaves;
   __shared__ float s_m[NW][16], s_l[NW][16];
-  __shared__ __attribute__((aligned(16))) float s_o[NW][16][kPitch];
+  // a wave's keys, and in their place its outputs when they are done with
+  constexpr size_t kKeyBytes = (size_t)kU * 16 * DP * sizeof(T), kOutBytes = sizeof(float) * 16 * kPitch, kWaveBytes = kKeyBytes > kOutBytes ? kKeyBytes : kOutBytes;
+  __shared__ __attribute__((aligned(16))) unsigned char s_raw[NW][kWaveBytes];
+  auto s_o = [&](int w) { return reinterpret_cast<float (*)[kPitch]>(s_raw[w]); };
   __shared__ typename Tile::QPart s_q[Tile::kSteps * Tile::kParts][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, c = lane & 15, d = a.c.d;
-  // Workgroups go to the XCDs in turn.  Heads come first and splits last: with the splits first, an XCD got one split of
-  // every sequence, and those of the last splits, which only long sequences have, little to do.  The blocks of a KV
-  // head's queries, which read the same rows, go to one XCD, one right after the other.
-  const unsigned octet = blockIdx.x / (8 * a.n_blocks), in_octet = blockIdx.x % (8 * a.n_blocks);
+  // Workgroups go to the XCDs in turn.  A layer of them, one per sequence and KV head, takes the same split of all; a layer
+  // begins an odd number of XCDs behind the one before, so that the splits of a sequence go round them all.  The last
+  // splits, which only long sequences have, come first.  The blocks of a KV head's queries, which read the same
+  // rows, go to one XCD, one right after the other.
+  const unsigned octet = blockIdx.x / (8 * a.n_blocks), in_octet = blockIdx.x % (8 * a.n_blocks), n_tasks = a.c.n_seqs * a.c.n_kv;
   const int hb = in_octet / 8;
-  unsigned id = octet * 8 + in_octet % 8;
-  const int hk = id % a.c.n_kv;
-  id /= a.c.n_kv;
-  const int seq = id % a.c.n_seqs, split = a.n_split - 1 - (int)(id / a.c.n_seqs);
-  if (split < 0) return;            // (the tasks are rounded up to a multiple of 8)
+  const unsigned id = octet * 8 + in_octet % 8, layer = id / n_tasks;
+  const unsigned task = (id - layer * n_tasks + (n_tasks & 1 ? 0 : layer)) % n_tasks;
+  const int split = a.n_split - 1 - (int)layer, seq = task / a.c.n_kv, hk = task - seq * a.c.n_kv;
+  if (split < 0) return;                     // (the tasks are rounded up to a multiple of 8)
   const int u_begin = split * a.split_units, u_wave = u_begin + wave * kU;
   const int G = a.n_q / a.c.n_kv, n_heads = min(16, G - 16 * hb);
   const size_t row0 = (size_t)seq * a.n_q + hk * G + 16 * hb;
@@ -328,7 +353,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_att
   };
   auto load_k = [&](int it) {
 #pragma unroll
-    for (int u = 0; u < kU; ++u) tile.load_k(u, (const char*)a.c.k + offset(it * kU + u), d, g, c);
+    for (int u = 0; u < kU; ++u) tile.k.load(u, (const char*)a.c.k + offset(it * kU + u), d * (int)sizeof(T), lane);
   };
   auto load_v = [&](int it) {
 #pragma unroll
@@ -352,11 +377,13 @@ __global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_att
   float m = -INFINITY, l = 0.f;
   for (int it = 0; it < n_it; ++it) {
     float x[Tile::kScores];
-    int q_lane = lane;
-    asm volatile("" : "+v"(q_lane));         // (else the queries are taken out of the loop, into registers)
-    tile.scores(s_q, q_lane, x);
+    u32x4_t* keys = reinterpret_cast<u32x4_t*>(s_raw[wave]);
+    tile.k.stage(keys, lane);
     const bool more = it + 1 < n_it;
     if (more) load_k(it + 1);
+    int q_lane = lane;
+    asm volatile("" : "+v"(q_lane));         // (else the queries are taken out of the loop, into registers)
+    Tile::scores(s_q, keys, q_lane, g, c, x);
     const int u0 = u_wave + it * (NW * kU);
     bool full = true;
 #pragma unroll
@@ -408,7 +435,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_att
 #pragma unroll
     for (int t = 0; t < Tile::kOut; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s_o[wave][c][Tile::out_col(t, 4 * g + r)] = o[t][r];
+      for (int r = 0; r < 4; ++r) s_o(wave)[c][Tile::out_col(t, 4 * g + r)] = o[t][r];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n_heads * (d / 4); i += 64 * NW) {
@@ -421,7 +448,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : 3) void paged_att
     for (int w = 0; w < NW; ++w) {
       const float f = s_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][h] - m_all);
       l_all += f * s_l[w][h];
-      v += f * *(const f32x4_t*)&s_o[w][h][e];
+      v += f * *(const f32x4_t*)&s_o(w)[h][e];
     }
     const size_t row = row0 + h;
     if (a.n_split > 1) {

@@ -321,7 +321,7 @@ int sv_advance_prefix(int32_t *prefix_len, const int32_t *accepted_len, int B, i
 
 /* probs[i][j] = exp(logits[i][j] / temperature) / sum over the row: what the heads' out_logits
  * become before sv_sampled_accept.  logits, probs: [device] float32 [n_rows, n_vocab]; probs may be
- * logits.  Maximum and sum are float32.  A row of nothing but -infinity (everything masked) becomes
+ * logits, and does not overlap it otherwise.  Maximum and sum are float32.  A row of nothing but -infinity (everything masked) becomes
  * zeros; a row that holds a NaN or +infinity becomes NaN.
  * SV_ERR_SHAPE unless 1 <= n_rows < 2^31 / 1024, 1 <= n_vocab <= SV_MAX_SAMPLED_VOCAB; SV_ERR_TOKEN unless
  * temperature is a number above zero, finite like its reciprocal (for the greedy choice there is sv_relaxed_accept). */

@@ -424,13 +424,13 @@ int sv_paged_workspace_bytes(const sv_paged_cache *cache, int n_q_heads, int max
  *     n_pages - 1 (such rows count as not visible), 0 otherwise
  *   workspace: [device], 256-byte aligned, ws_bytes >= sv_paged_workspace_bytes
  * A sequence without visible rows (length 0) gets zeros and lse = -infinity.  Rows that are not visible may
- * hold anything, NaN and infinity too.  A NaN or infinity in a visible row or a query makes at most
- * the outputs of the heads that read it NaN or infinite; which of the two is not specified.
+ * hold anything, NaN and infinity too.  A NaN or infinity in a visible row or a query reaches
+ * the outputs of the heads that read it and no others; whether as a NaN, an infinity or not at all is not specified.
  * Scores, softmax and outputs are float32; with a bf16 cache queries and weights enter the matrix
  * cores as sums of three bf16 numbers (2^-24 of each value).  Results are the same in every run.
  * SV_ERR_DTYPE for other cache types; SV_ERR_SHAPE if a size or alignment is outside the rules
  * above, n_q_heads is no multiple of n_kv_heads, n_seqs or n_q_heads exceeds 2^15, max_pages *
- * page_size 2^30, or scale is not finite; SV_ERR_WORKSPACE if the scratch is too small or misaligned. */
+ * page_size 2^30, n_seqs * n_q_heads * ceil(max_len / 4096) 2^23, or scale is not finite; SV_ERR_WORKSPACE if the scratch is too small or misaligned. */
 int sv_paged_attention(const sv_paged_cache *cache, const int32_t *seq_len, int max_len,
                        const float *q, int n_q_heads, float scale, int window, int n_sink,
                        float *out, float *lse, int32_t *status, void *workspace, size_t ws_bytes,

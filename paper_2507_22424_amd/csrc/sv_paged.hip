@@ -22,7 +22,10 @@ static PagedCache view(const sv_paged_cache& c) {
 
 static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   if (n_q < 1 || n_q > (1 << 15) || n_q % c.n_kv_heads || max_len < 0 || max_len > c.max_pages * c.page_size) return SV_ERR_SHAPE;
-  return SV_OK;
+  // a launch has less than 2^32 threads: 256 for a piece of a row at most, which has 4096 rows of the cache at least where
+  // there are many, and 64 x 32 for a row that is joined from more than eight
+  const long long pieces = (max_len + 4095ll) / 4096;
+  return (long long)c.n_seqs * n_q * (pieces > 1 ? pieces : 1) > (1ll << 23) ? SV_ERR_SHAPE : SV_OK;
 }
 
 // How a call is split over the chip, in workgroups' rounds (a tile for each of the four waves: 128 rows of a bf16

@@ -97,6 +97,13 @@ def test_paged_attention_refusals():
     assert sv.lib().sv_paged_workspace_bytes(C.byref(view), 4, 65536, C.byref(n)) == 0 and n.value > 256
     assert _attend(view, max_len=65536, ws_bytes=n.value - 1) == -5 and _attend(view, max_len=65536, ws=C.c_void_p(4096 + 128)) == -5
     assert sv.lib().sv_paged_workspace_bytes(C.byref(view), 4, 65536, None) == -1
+    # more threads than a launch can have: n_seqs * n_q_heads * ceil(max_len / 4096) above 2^23
+    for seqs, n_q, length, ok in ((1 << 15, 256, 4096, True), (1 << 15, 258, 4096, False), (1 << 15, 256, 4097, False), (1 << 15, 256, 0, True),
+                                  (1 << 10, 32, 1 << 20, True), (1 << 10, 34, 1 << 20, False)):
+        view = _view(max_pages=1 << 16, n_seqs=seqs)
+        assert sv.lib().sv_paged_workspace_bytes(C.byref(view), n_q, length, C.byref(n)) == (0 if ok else -2), (seqs, n_q, length)
+        if not ok:
+            assert _attend(view, n_q=n_q, max_len=length) == -2
 
 
 @pytest.mark.parametrize("n_seqs,n_kv,n_q,d", [(1, 1, 1, 64), (1, 8, 32, 128), (3, 2, 80, 256), (64, 8, 32, 128), (700, 5, 35, 96)])

@@ -112,7 +112,11 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
 // by readlane, and the branches are uniform over the workgroup.  Only sums over whole rows (before a second
 // sibling, and for the draw) read the rows.
 // Sums are float64: the inputs are float32, so that a sum is exact unless its terms span more
-// than 2^29, and the choice of a token does not hang on the order of the summation.
+// than 2^29, and the choice of a token does not hang on the order of the summation.  They go from lane to lane by
+// data-parallel primitives (through LDS, and with every wave adding up all waves' parts by itself, 16 trees over
+// 4000 columns took 26.6 us, now 11.7).  Bound by what one CU fetches, some 50 - 60 bytes a nanosecond: 128 chains over
+// 128259 columns 32 us for 131 MB, where 20 would be the memory's time.  A tree over 256 columns, 5.4 us, is a chain of
+// loads: tree, probabilities of the tokens, the last row.
 
 struct SampleArgs {
   const int32_t* parent;
@@ -124,10 +128,30 @@ struct SampleArgs {
   int32_t *accepted_len, *best_node, *path, *out_tokens, *status;
 };
 
-__device__ inline double wave_sum_f64(double v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-  return v;
+// The value of another lane by data-parallel primitive, 0 from where there is none.
+template <int kCtrl, int kRows>
+__device__ inline double dpp_f64(double v) {
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  const u32x2_t r = {(unsigned)__builtin_amdgcn_update_dpp(0, (int)w[0], kCtrl, kRows, 0xf, false),
+                     (unsigned)__builtin_amdgcn_update_dpp(0, (int)w[1], kCtrl, kRows, 0xf, false)};
+  return __builtin_bit_cast(double, r);
+}
+// Sums up to each lane: of the first 16 lanes, of all.
+__device__ inline double row_scan_f64(double v) {
+  v += dpp_f64<0x111, 0xf>(v);               // row_shr:1, 2, 4, 8
+  v += dpp_f64<0x112, 0xf>(v);
+  v += dpp_f64<0x114, 0xf>(v);
+  return v + dpp_f64<0x118, 0xf>(v);
+}
+__device__ inline double wave_scan_f64(double v) {
+  v = row_scan_f64(v);
+  v += dpp_f64<0x142, 0xa>(v);               // row_bcast:15 to rows 1 and 3, row_bcast:31 to rows 2 and 3
+  return v + dpp_f64<0x143, 0xc>(v);
+}
+__device__ inline double lane_f64(double v, int lane) {
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  const u32x2_t r = {(unsigned)__builtin_amdgcn_readlane((int)w[0], lane), (unsigned)__builtin_amdgcn_readlane((int)w[1], lane)};
+  return __builtin_bit_cast(double, r);
 }
 
 __device__ inline float mass_of(float p) { return fmaxf(p, 0.f); }       // (a NaN has none)
@@ -190,75 +214,64 @@ struct RowSearch {
   __device__ void sums(const RestOfRow& row, int begin, int end, int run) {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int first = begin + wave * run, stop = min(end, first + run);
-    const double s = wave_sum_f64(row.less != 0.0 ? lane_sum<true>(row, first, stop) : lane_sum<false>(row, first, stop));
+    const double s = wave_scan_f64(row.less != 0.0 ? lane_sum<true>(row, first, stop) : lane_sum<false>(row, first, stop));
+    publish(wave, s);
+  }
+  // the sum up to lane 63 of each wave -> part
+  __device__ void publish(int wave, double upto) {
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[wave] = s;
+    if ((threadIdx.x & 63) == 63) part[wave] = upto;
     __syncthreads();
   }
   __device__ static int run_of(int n) { return (n + kWaves - 1) / kWaves; }
+  __device__ double my_part() const { return (threadIdx.x & 63) < kWaves ? part[threadIdx.x & 63] : 0.0; }
   // (leaves the runs' sums in part)
   __device__ double total(const RestOfRow& row, int n) {
     sums(row, 0, n, run_of(n));
-    double s = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s += part[w];
-    return s;
+    return lane_f64(row_scan_f64(my_part()), 15);
   }
   // First column with mass at which the cumulated sum exceeds goal, the last one with mass if there is
   // none.  After total(row, n).
   __device__ int find(const RestOfRow& row, int n, double goal) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     int begin = 0, end = n;
     double before = 0.0;
-    while (end - begin > NT * kLeaf) {
+    while (kWaves > 1 && end - begin > NT * kLeaf) {       // (one wave is for rows of up to 64 kLeaf columns: it could not cut them)
       const int run = run_of(end - begin);
       if (end - begin < n) sums(row, begin, end, run);
-      int in = 0;
-      bool found = false;
-      double cum = before, at = before;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const bool here = (part[w] > 0.0) & !found;
-        in = here ? w : in;
-        at = here ? cum : at;
-        cum += part[w];
-        found = found | (here & (cum > goal));
-      }
-      before = at;
+      const double mine = my_part(), upto = row_scan_f64(mine);
+      const unsigned long long some = __builtin_amdgcn_ballot_w64(mine > 0.0), over = some & __builtin_amdgcn_ballot_w64(before + upto > goal);
+      const int in = over ? __builtin_ctzll(over) : (some ? 63 - __builtin_clzll(some) : 0);
+      if (in) before += lane_f64(upto, in - 1);
       begin += in * run;
       end = min(end, begin + run);
     }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = begin + kLeaf * (int)threadIdx.x;
+    const int first = begin + kLeaf * (int)threadIdx.x;
     double v[kLeaf], mine = 0.0;
     if (row.less != 0.0) rest_at<kLeaf, 1, true, false>(row, first, end, v);
     else rest_at<kLeaf, 1, false, false>(row, first, end, v);
 #pragma unroll
     for (int k = 0; k < kLeaf; ++k) mine += v[k];
-    double upto = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const double o = __shfl_up(upto, off, kWave);
-      if (lane >= off) upto += o;
-    }
-    __syncthreads();
-    if (lane == 63) part[wave] = upto;
+    const double upto = wave_scan_f64(mine);
     if (threadIdx.x == 0) {
       hit = n;
       last = 0;
     }
-    __syncthreads();
-    double cum = before + (upto - mine);
-    for (int w = 0; w < wave; ++w) cum += part[w];
+    publish(wave, upto);
+    const double waves = row_scan_f64(my_part());
+    double cum = before + (wave ? lane_f64(waves, wave - 1) : 0.0) + (upto - mine);
     int my_hit = n, my_last = -1;
-#pragma unroll
-    for (int k = kLeaf - 1; k >= 0; --k)
-      if (v[k] > 0.0 && my_last < 0) my_last = first + k;
 #pragma unroll
     for (int k = 0; k < kLeaf; ++k) {
       cum += v[k];
-      if (v[k] > 0.0 && cum > goal && my_hit == n) my_hit = first + k;
+      const bool some = v[k] > 0.0;
+      my_hit = some & (cum > goal) & (my_hit == n) ? first + k : my_hit;
+      my_last = some ? first + k : my_last;
     }
-    if (my_hit < n) atomicMin(&hit, my_hit);
-    if (my_last >= 0) atomicMax(&last, my_last);
+    // (columns rise with the lanes)
+    const unsigned long long hits = __builtin_amdgcn_ballot_w64(my_hit < n), lasts = __builtin_amdgcn_ballot_w64(my_last >= 0);
+    if (hits && lane == __builtin_ctzll(hits)) atomicMin(&hit, my_hit);
+    if (lasts && lane == 63 - __builtin_clzll(lasts)) atomicMax(&last, my_last);
     __syncthreads();
     return hit < n ? hit : last;
   }

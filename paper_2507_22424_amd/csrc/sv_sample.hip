@@ -10,6 +10,9 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
   if (n_rows < 1 || n_rows >= (1 << 21) || n_vocab < 1 || n_vocab > SV_MAX_SAMPLED_VOCAB) return SV_ERR_SHAPE;
   const float inv_t = 1.f / temperature, c = (float)(1.4426950408889634 / (double)temperature);
   if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t) || !std::isfinite(c)) return SV_ERR_TOKEN;
+  // Threads and columns a thread keeps, by the length of a row (us, 60 and 2000 or 960 rows: 256 columns 64 x 4 2.4, 3.0, 256 x 8
+  // 2.6, 4.3; 2000 columns 256 x 8 2.8, 6.7, 1024 x 8 3.4, 13.8; 8000 columns 1024 x 8 3.7, 12.2, 1024 x 32 5.9, 22.7;
+  // 32000 columns 1024 x 32 6.8, 42.7, two reads 9.0, 52.2).
   if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, c, probs);
   else if (n_vocab <= 2048) token_probs_kernel<256, 8><<<n_rows, 256, 0, st>>>(logits, n_vocab, c, probs);
   else if (n_vocab <= 8192) token_probs_kernel<1024, 8><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);
@@ -23,10 +26,15 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
 }
 
 static int sampled_accept(const SampleArgs& a, int B, hipStream_t st) {
+  // Threads by the length of a row (16 trees of 60 drawn tokens, us with 64 or 128 / 256 / 512 / 1024: 1000 columns 9.9 / 10.5 /
+  // 12.7 / 18.0, 2000 10.9 / 9.3 / 11.6 / 16.1, 4000 - / 11.7 / 11.6 / 17.9, 8000 - / 17.3 / 15.5 / 17.4, 32000 - / 38.1 / 28.2 / 28.9;
+  // 128 chains of 128259: 56.0 / 32.9 / 32.1).  One wave takes 256 columns at most, see RowSearch::find.
   auto run = [&](auto drawn) {
     constexpr bool kDrawn = decltype(drawn)::value;
     if (a.n_vocab <= 256) sampled_accept_kernel<64, kDrawn><<<B, 64, 0, st>>>(a);
-    else if (a.n_vocab <= 2048) sampled_accept_kernel<256, kDrawn><<<B, 256, 0, st>>>(a);
+    else if (a.n_vocab <= 1024) sampled_accept_kernel<128, kDrawn><<<B, 128, 0, st>>>(a);
+    else if (a.n_vocab <= 4096) sampled_accept_kernel<256, kDrawn><<<B, 256, 0, st>>>(a);
+    else if (a.n_vocab <= 16384) sampled_accept_kernel<512, kDrawn><<<B, 512, 0, st>>>(a);
     else sampled_accept_kernel<1024, kDrawn><<<B, 1024, 0, st>>>(a);
   };
   if (a.draft) run(std::true_type{});

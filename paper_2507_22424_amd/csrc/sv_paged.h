@@ -477,9 +477,9 @@ __global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : (DP == 128 && siz
 }
 
 // Joins the splits of a row.  A thread has four columns of it and every J-th split; the J sums are added in order
-// through LDS.  J = 1 up to eight splits, whose loads a thread has under way together.  Behind the workgroups that
+// through LDS.  J = 1 up to kMost splits, whose loads a thread has under way together.  Behind the workgroups that
 // join (grid: ceil(rows * d / 4 / (256 / J))) come one per sequence that look over its pages for the status.
-template <int J>
+template <int J, int kMost>
 __global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs a, unsigned n_join) {
   constexpr int kCols = 256 / J;             // columns (of four) of a workgroup
   __shared__ float s_l[J][kCols];
@@ -507,7 +507,6 @@ __global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs 
   float m = -INFINITY, l = 0.f;
   f32x4_t v = {0.f, 0.f, 0.f, 0.f};
   if constexpr (J == 1) {
-    constexpr int kMost = 8;
     float2 e[kMost];
     f32x4_t w[kMost];
 #pragma unroll

@@ -31,11 +31,12 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
 // How a call is split over the chip, in workgroups' rounds (a tile for each of the four waves: 128 rows of a bf16
 // cache, 64 of a float32 one).  Up to one workgroup per CU a piece may be as short as a round, if there are three
 // pieces at least (the second launch, which joins them, takes 4 us): 600 tokens, 8 KV heads, 11.4 us in one piece, 9.3 in four.
-// Beyond, a piece has four rounds (32 sequences of up to 1000 tokens: 18.7 us in one piece, 21.3 in three, 24.5 in six),
-// and there are as many as run at a time (three per CU), or four times as many for several sequences, some of which
-// are shorter than others (64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in 3072).  A piece has a unit of 16 rows at least
-// for each query head of a KV head, beside whose rows its results would not be little.
-// Splits (and with them the scratch) never get fewer as max_len grows.
+// Pieces of more than ten rounds are cut further, into pieces of four: until as many run as can at a time (three per CU),
+// or four times as many for several sequences, some of which are shorter than others (24 float32 sequences of up to 1500
+// tokens, 11.8 rounds: 17.7 us in two pieces, 15.2 in five; 64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in 3072; but 48 of
+// 1028 visible tokens, 8.3 rounds: 18.9 us in one, 21.5 in two, and 4 float32 ones of up to 3000, 18.1 us in eight, 24.0 in
+// eleven).  A piece has a unit of 16 rows at least for each query head of a KV head, beside whose rows its results would
+// not be little.  Splits (and with them the scratch) never get fewer as max_len grows.
 constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 3072;
 constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
@@ -51,10 +52,10 @@ static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
     const int fill = n_units / (G > least_units ? G : least_units);
     return fill < least_pieces ? 1 : (int)(fill < most ? fill : most);
   };
-  p.n_split = 1;
-  for (const int n : {pieces(kGroupsSmall / tasks, round, 3), pieces(ceil_div(c.n_seqs > 1 ? kGroupsRagged : kGroupsOne, tasks), 4 * round, 2),
-                      ceil_div(n_units, kPagedWaves * kBatchUnits)})
-    p.n_split = n > p.n_split ? n : p.n_split;
+  p.n_split = pieces(kGroupsSmall / tasks, round, 3);
+  if (p.n_split < 1) p.n_split = 1;
+  const int cut = ceil_div(n_units, p.n_split) > 10 * round ? pieces(ceil_div(c.n_seqs > 1 ? kGroupsRagged : kGroupsOne, tasks), 4 * round, 2) : 1;
+  for (const int n : {cut, ceil_div(n_units, kPagedWaves * kBatchUnits)}) p.n_split = n > p.n_split ? n : p.n_split;
   p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
   p.rows = (size_t)c.n_seqs * n_q;
   p.part = 0;
@@ -148,9 +149,9 @@ int sv_paged_attention(const sv_paged_cache* cache, const int32_t* seq_len, int 
   if (past_caches(*cache, p, units)) typed(std::integral_constant<int, 1>{});
   else typed(std::integral_constant<int, 0>{});
   if (p.n_split > 1) {
-    const int joiners = p.n_split <= 8 ? 1 : 32;
+    const int joiners = p.n_split <= 16 ? 1 : 32;
     const unsigned n_join = (unsigned)((p.rows * (cache->head_dim / 4) * joiners + 255) / 256);
-    auto join = joiners == 1 ? paged_attention_join<1> : paged_attention_join<32>;
+    auto join = p.n_split <= 8 ? paged_attention_join<1, 8> : (p.n_split <= 16 ? paged_attention_join<1, 16> : paged_attention_join<32, 0>);
     join<<<n_join + (status ? cache->n_seqs : 0), 256, 0, st>>>(a, n_join);
   }
   return launch_status();

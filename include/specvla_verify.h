@@ -349,8 +349,8 @@ int sv_token_probs(const float *logits, int n_rows, int n_vocab, float temperatu
  *   draft_token:  [device] int32[B*T] (entry 0 of each tree unused)
  *   target_prob, draft_prob: [device] float32 [B*T, n_vocab], columns = token ids vocab_lo ..
  *     vocab_lo + n_vocab - 1, rows taken as normalised (sv_token_probs); draft_prob may be NULL.
- *     Rows of nodes that the walk does not reach are not read.  A token outside the columns has p = q = 0:
- *     it is never accepted.  A NaN or a negative number counts as 0.
+ *     Rows of nodes that the walk does not reach have no effect (all that is read of them are the columns
+ *     of the node's children).  A token outside the columns has p = q = 0: it is never accepted.  A NaN or a negative number counts as 0.
  *   u_accept: [device] float32[B*T], u_draw: [device] float32[B]: uniform numbers in [0, 1)
  *   accept_mask, accepted_len, best_node, path, out_tokens: [device, out] as sv_relaxed_accept
  *     leaves them (accept_mask is 1 on the path only), so that sv_commit_path and sv_advance_prefix

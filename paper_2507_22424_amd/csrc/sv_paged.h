@@ -205,9 +205,14 @@ struct PagedTile<bf16_t, DP, NT> {
 
   static __device__ int out_col(int t, int m) { return t / kE * 16 * kE + kE * m + t % kE; }
   static __device__ void load_q(int s, const float* src, bool real, float scale, int d, int g, QPart* part) {
+    // (loaded whether wanted or not: a load under a condition is waited for before the next)
+    const int col = 32 * s + 8 * g;
+    const f32x4_t* at = (const f32x4_t*)(src + min(col, d - 8));
+    const f32x4_t a = at[0], b = at[1];
+    const bool want = real & (col < d);
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = real && 32 * s + 8 * g < d ? src[32 * s + 8 * g + e] * scale : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = want ? (e < 4 ? a[e & 3] : b[e & 3]) * scale : 0.f;
     split8_3(x, part);
   }
   __device__ void load_v(int u, const char* base, int d, int g, int c) {
@@ -275,8 +280,11 @@ struct PagedTile<float, DP, NT> {
 
   static __device__ int out_col(int t, int m) { return t / 4 * 64 + 4 * m + t % 4; }
   static __device__ void load_q(int s, const float* src, bool real, float scale, int d, int g, QPart* part) {
+    const int col = 16 * s + 4 * g;
+    const f32x4_t a = *(const f32x4_t*)(src + min(col, d - 4));
+    const bool want = real & (col < d);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part[0][e] = real && 16 * s + 4 * g < d ? src[16 * s + 4 * g + e] * scale : 0.f;
+    for (int e = 0; e < 4; ++e) part[0][e] = want ? a[e] * scale : 0.f;
   }
   __device__ void load_v(int, const char* base, int d, int g, int c) {
 #pragma unroll

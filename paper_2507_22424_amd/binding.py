@@ -469,11 +469,12 @@ def _opt(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, name: str) 
 
 
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+_I32_MAX = (1 << 31) - 1       # (ctypes takes a larger number modulo 2^32 for an int, without a word)
 
 
 def sv_token_probs(logits: torch.Tensor, temperature: float, probs: torch.Tensor, stream=None) -> None:
     """probs = softmax(logits / temperature) of [rows, vocabulary]; `probs` may be `logits`."""
-    if logits.dim() != 2 or probs.shape != logits.shape:
+    if logits.dim() != 2 or probs.shape != logits.shape or max(logits.shape) > _I32_MAX:
         raise ValueError("token_probs: logits and probs must be [rows, vocabulary]")
     dev = _device()
     rc = lib().sv_token_probs(_ptr(logits, _F32, dev, "logits"), *logits.shape, temperature, _ptr(probs, _F32, dev, "probs"),
@@ -488,7 +489,7 @@ def sv_sampled_accept(tree: Tree, draft_token: torch.Tensor, target_prob: torch.
                       out_tokens: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """target_prob, draft_prob: [B*T, columns]; the other sizes as in sv_relaxed_accept."""
     n, n_vocab = B * tree.n_nodes, target_prob.shape[-1]
-    if target_prob.numel() != n * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
+    if max(n_vocab, abs(vocab_lo), d_cap) > _I32_MAX or target_prob.numel() != n * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
             draft_token.numel() != n or u_accept.numel() != n or u_draw.numel() != B or accept_mask.numel() != n or \
             accepted_len.numel() != B or best_node.numel() != B or status.numel() != B or \
             path.numel() != B * (d_cap + 1) or out_tokens.numel() != B * (d_cap + 1):
@@ -535,6 +536,8 @@ def sv_paged_append(cache: "PagedCache", token_seq: torch.Tensor, token_pos: tor
 
 
 def sv_paged_workspace_bytes(cache: "PagedCache", n_q_heads: int, max_len: int) -> int:
+    if not -_I32_MAX <= min(n_q_heads, max_len) <= max(n_q_heads, max_len) <= _I32_MAX:
+        raise ValueError("paged_workspace_bytes: n_q_heads and max_len must be 32-bit numbers")
     out = C.c_size_t(0)
     _check(lib().sv_paged_workspace_bytes(C.byref(cache.struct), n_q_heads, max_len, C.byref(out)),
            "sv_paged_workspace_bytes")
@@ -545,12 +548,15 @@ def sv_paged_attention(cache: "PagedCache", seq_len: torch.Tensor, max_len: int,
                        window: int, n_sink: int, out: torch.Tensor, lse: Optional[torch.Tensor],
                        status: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     """q, out: [sequences, query heads, head_dim] float32; window 0: every row is visible."""
-    c, dev = cache.struct, _device()
+    c = cache.struct
     n_seqs = c.n_seqs
     if q.dim() != 3 or q.shape[0] != n_seqs or q.shape[2] != c.head_dim or out.shape != q.shape or \
             seq_len.numel() != n_seqs or (lse is not None and lse.numel() != n_seqs * q.shape[1]) or \
             (status is not None and status.numel() != n_seqs):
         raise ValueError("paged_attention: tensor sizes do not match the cache")
+    if not -_I32_MAX <= min(max_len, window, n_sink) <= max(max_len, window, n_sink) <= _I32_MAX:
+        raise ValueError("paged_attention: max_len, window and n_sink must be 32-bit numbers")
+    dev = _device()
     cache.check_device(dev)
     rc = lib().sv_paged_attention(
         C.byref(c), _ptr(seq_len, _I32, dev, "seq_len"), max_len, _ptr(q, _F32, dev, "q"), q.shape[1], scale, window, n_sink,

@@ -122,3 +122,23 @@ def test_the_holder_refuses_tensors_that_are_no_cache():
               (k, k, table)):                       # the last: on the host
         with pytest.raises(ValueError):
             sv.PagedCache(*a)
+
+
+def test_numbers_past_32_bits_are_refused():
+    """Not taken modulo 2^32, as an int argument of the C call would be."""
+    cache = type("Cache", (), {"struct": _view(n_seqs=1, n_kv_heads=2, head_dim=64, max_pages=4)})()
+    q, ws, one = torch.zeros(1, 2, 64), torch.zeros(256, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)
+    big = 1 << 32
+    for max_len, window, n_sink in ((big + 5, 0, 0), (5, big, 0), (5, big + 4, 0), (5, 3, big + 1), (-big + 5, 0, 0), (5, -big, 0)):
+        with pytest.raises(ValueError, match="32-bit"):
+            sv.sv_paged_attention(cache, one, max_len, q, 0.1, window, n_sink, q, None, None, ws)
+    for n_q, max_len in ((big + 2, 5), (2, big + 5)):
+        with pytest.raises(ValueError, match="32-bit"):
+            sv.sv_paged_workspace_bytes(cache, n_q, max_len)
+    wide = torch.zeros(1, 1).expand(big + 1, 1)
+    with pytest.raises(ValueError, match="rows, vocabulary"):
+        sv.sv_token_probs(wide, 1.0, wide)
+    tree, nodes, out = sv.Tree(4096, 4096, 4096, 2, 1), torch.zeros(2), torch.zeros(8, dtype=torch.int32)
+    for p, lo in ((torch.zeros(1, 1).expand(2, big + 1), 0), (torch.zeros(2, 5), big), (torch.zeros(2, 5), -big)):
+        with pytest.raises(ValueError, match="sizes"):
+            sv.sv_sampled_accept(tree, nodes.int(), p, None, lo, nodes, nodes[:1], 1, 7, nodes.byte(), out[:1], out[:1], out, out, out[:1])

@@ -84,10 +84,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
 // and joins the waves.  Units are 16 rows of a page at a multiple of 16, so that a unit lies in one page.
 //
 // Bound by the cache's rows from memory.  A wave has the next tile's K under way while it works on a tile, and the next V
-// from its end on; three workgroups of four waves share a CU (head_dim 128: 166 registers).  64 sequences of 17 - 8192
-// tokens, 32 query and 8 KV heads of 128, bf16: 183 us for 1.08 GB, 5.9 TB/s (a plain streaming read: 6.7); one
+// from its end on; three workgroups of four waves share a CU (head_dim 128: 167 registers).  64 sequences of 17 - 8192
+// tokens, 32 query and 8 KV heads of 128, bf16: 182 us for 1.08 GB, 5.9 TB/s (a plain streaming read: 6.7); one
 // of 131071: 92 us for 537 MB, 5.8 TB/s.  With little to read it is the chain of loads: 281 tokens, 32 heads,
-// 8.5 us, of which an empty kernel takes 2.0, queries, length and pages 1.6, the first tile 1.8, two more 1.6 each.
+// 8.1 us, of which an empty kernel takes 2.0, the first tile with all that it waits for 2.9, two more 1.6 each.
 // 32-bit sums: queries and weights enter the bf16 products in three parts, which is all of their 24 bits.
 
 struct PagedAttnArgs {

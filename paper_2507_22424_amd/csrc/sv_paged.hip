@@ -33,11 +33,11 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
 // pieces at least (the second launch, which joins them, takes 4 us): 600 tokens, 8 KV heads, 11.4 us in one piece, 9.3 in four.
 // Pieces of more than ten rounds are cut further, into pieces of four: until as many run as can at a time (three per CU),
 // or four times as many for several sequences, some of which are shorter than others (24 float32 sequences of up to 1500
-// tokens, 11.8 rounds: 17.7 us in two pieces, 15.2 in five; 64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in 3072; but 48 of
+// tokens, 11.8 rounds: 17.7 us in two pieces, 15.2 in five; 64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in three times as many; but 48 of
 // 1028 visible tokens, 8.3 rounds: 18.9 us in one, 21.5 in two, and 4 float32 ones of up to 3000, 18.1 us in eight, 24.0 in
 // eleven).  A piece has a unit of 16 rows at least for each query head of a KV head, beside whose rows its results would
 // not be little.  Splits (and with them the scratch) never get fewer as max_len grows.
-constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 3072;
+constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 4 * kGroupsOne;
 constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
   int n_blocks, n_split, split_units;

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
 // than 2^29, and the choice of a token does not hang on the order of the summation.  They go from lane to lane by
 // data-parallel primitives (through LDS, and with every wave adding up all waves' parts by itself, 16 trees over
 // 4000 columns took 26.6 us, now 11.7).  Bound by what one CU fetches, some 50 - 60 bytes a nanosecond: 128 chains over
-// 128259 columns 32 us for 131 MB, where 20 would be the memory's time.  A tree over 256 columns, 5.4 us, is a chain of
+// 128259 columns 33 us for 131 MB, where 20 would be the memory's time.  A tree over 256 columns, 5.3 us, is a chain of
 // loads: tree, probabilities of the tokens, the last row.
 
 struct SampleArgs {

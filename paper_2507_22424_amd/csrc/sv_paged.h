@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256) void paged_attention_join(const PagedAttnArgs 
     }
 #pragma unroll
     for (int s = 0; s < kMost; ++s) {
-      const float f = (s < n) & (e[s].x != -INFINITY) ? __builtin_amdgcn_exp2f(e[s].x - m) : 0.f;
+      const float f = ((s < n) & (e[s].x != -INFINITY)) ? __builtin_amdgcn_exp2f(e[s].x - m) : 0.f;
       l += f * e[s].y;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] += f == 0.f ? 0.f : f * w[s][k];

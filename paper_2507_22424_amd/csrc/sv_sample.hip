@@ -26,16 +26,20 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
 }
 
 static int sampled_accept(const SampleArgs& a, int B, hipStream_t st) {
-  // Threads by the length of a row (16 trees of 60 drawn tokens, us with 64 or 128 / 256 / 512 / 1024: 1000 columns 9.9 / 10.5 /
-  // 12.7 / 18.0, 2000 10.9 / 9.3 / 11.6 / 16.1, 4000 - / 11.7 / 11.6 / 17.9, 8000 - / 17.3 / 15.5 / 17.4, 32000 - / 38.1 / 28.2 / 28.9;
-  // 128 chains of 128259: 56.0 / 32.9 / 32.1).  One wave takes 256 columns at most, see RowSearch::find.
+  // Threads by the length of a row (16 trees of 60 drawn tokens, us with 64 / 128 / 256 / 512 / 1024: 200 columns 6.1 / 6.9, 1000
+  // - / 7.8 / 8.4, 2000 - / 9.1 / 7.7, 4000 - / - / 9.9 / 12.3, 8000 - / - / 14.4 / 12.3, 16000 - / - / - / 14.3 / 15.0; not held: 128 chains
+  // of 128259 - / - / 56.0 / 32.9 / 32.1).  One wave takes 256 columns at most, see RowSearch::find.
+  // Rows held take 128 KB of LDS for 1024 threads, so that one workgroup is on a CU instead of two: 400 trees of 32000
+  // columns 57 us unheld, 42 held, but 1000 of 20000 78 and 86, 1000 chains 54 and 64.
   auto run = [&](auto drawn) {
     constexpr bool kDrawn = decltype(drawn)::value;
-    if (a.n_vocab <= 256) sampled_accept_kernel<64, kDrawn><<<B, 64, 0, st>>>(a);
-    else if (a.n_vocab <= 1024) sampled_accept_kernel<128, kDrawn><<<B, 128, 0, st>>>(a);
-    else if (a.n_vocab <= 4096) sampled_accept_kernel<256, kDrawn><<<B, 256, 0, st>>>(a);
-    else if (a.n_vocab <= 16384) sampled_accept_kernel<512, kDrawn><<<B, 512, 0, st>>>(a);
-    else sampled_accept_kernel<1024, kDrawn><<<B, 1024, 0, st>>>(a);
+    if (a.n_vocab <= 256) sampled_accept_kernel<64, kDrawn, kDrawn><<<B, 64, 0, st>>>(a);
+    else if (a.n_vocab <= 1024) sampled_accept_kernel<128, kDrawn, kDrawn><<<B, 128, 0, st>>>(a);
+    else if (a.n_vocab <= 4096) sampled_accept_kernel<256, kDrawn, kDrawn><<<B, 256, 0, st>>>(a);
+    else if (a.n_vocab <= 16384) sampled_accept_kernel<512, kDrawn, kDrawn><<<B, 512, 0, st>>>(a);
+    else if (kDrawn && B <= 512 && a.n_vocab <= 1024 * HeldRow<1024>::kColumns)
+      sampled_accept_kernel<1024, kDrawn, kDrawn><<<B, 1024, 0, st>>>(a);
+    else sampled_accept_kernel<1024, kDrawn, false><<<B, 1024, 0, st>>>(a);
   };
   if (a.draft) run(std::true_type{});
   else run(std::false_type{});

@@ -244,6 +244,56 @@ def test_sampled_accept_reads_only_rows_of_the_walk_and_is_reproducible():
     assert all(torch.equal(x, y) for x, y in zip(keep, [t for t in args if torch.is_tensor(t)]))
 
 
+@pytest.mark.parametrize("V", [256, 257, 1024, 1025, 4096, 4097, 16384, 16385, 32768, 32769])
+def test_sampled_accept_of_many_refused_siblings(V):
+    """Several sums over one row, at every node of the walk: random numbers near 1 refuse nearly all but the last of a
+    node's children.  Lengths at which more threads take a row, and one that none hold."""
+    rng = np.random.default_rng(V)
+    parents = [[-1, 0, 0, 0, 0, 4, 4, 4, 7, 7, 7, 7], [-1, 0, 0, 0, 0, 0, 0, 1, 1, 6, 6, 6]]
+    B, T = 2, 12
+    a = Accept(parents, 6)
+    for trial in range(3):
+        p, q = _probs(rng, (B, T, V), 1.0), _probs(rng, (B, T, V), 1.0)
+        tok = _draft_tokens(parents, q.astype(np.float64), rng, True)
+        u = np.full((B, T), 0.999, dtype=np.float32)
+        if trial:                                    # and the walk goes on behind a node's last child
+            u[0, [4, 7]] = 0.0
+            u[1, [6, 11]] = 0.0
+        if trial == 2:
+            p[0, 0, V // 2:] = np.nan                # has no mass
+            q[:, 7, ::3] = np.nan
+        a.check(tok, np.nan_to_num(p, nan=0.0), np.nan_to_num(q, nan=0.0), 0, u, rng.random(B).astype(np.float32))
+        dev = lambda x, dt: torch.from_numpy(x).to(dt).cuda()
+        want = [t.clone() for t in a.outputs()]
+        ud = torch.tensor([0.25, 0.75], device="cuda")
+        outs = []
+        for pp, qq in ((p, q), (np.nan_to_num(p, nan=0.0), np.nan_to_num(q, nan=0.0))):
+            a.call(dev(tok.reshape(-1), torch.int32), dev(pp.reshape(B * T, V), torch.float32), dev(qq.reshape(B * T, V), torch.float32), 0,
+                   dev(u.reshape(-1), torch.float32), ud)
+            outs.append([t.clone() for t in a.outputs()])
+        assert all(torch.equal(x, y) for x, y in zip(*outs))
+        assert torch.equal(want[0], outs[0][0])      # what is accepted does not hang on the draw
+
+
+def test_sampled_accept_of_many_trees_is_that_of_few():
+    """600 trees over rows that the workgroups of few trees hold."""
+    rng = np.random.default_rng(3)
+    few, n, T, V = 8, 600, 5, 16500
+    p, q = _probs(rng, (few, T, V), 1.0), _probs(rng, (few, T, V), 1.0)
+    u, ud = rng.random((few, T)).astype(np.float32), rng.random(few).astype(np.float32)
+    parents = [[-1, 0, 0, 0, 3]] * few
+    tok = _draft_tokens(parents, q.astype(np.float64), rng, True)
+    a = Accept(parents, 3)
+    a.check(tok, p, q, 0, u, ud)
+    many = Accept([parents[0]] * n, 3)
+    at = torch.arange(n, device="cuda") % few
+    dev = lambda x, dt: torch.from_numpy(x).to(dt).cuda()[at]
+    many.call(dev(tok, torch.int32).reshape(-1), dev(p, torch.float32).view(n * T, V), dev(q, torch.float32).view(n * T, V), 0,
+              dev(u, torch.float32).reshape(-1), dev(ud, torch.float32))
+    for x, y in zip(many.outputs(), a.outputs()):
+        assert torch.equal(x.view(n, -1), y.view(few, -1)[at])
+
+
 # ---- append ---------------------------------------------------------------------------------------
 
 def _append_case(dtype, nq, nkv, d, page, max_pages, seqs, pos, theta=1e4, table=None, n_seqs=None, fused=True, with_q=True, in_place=False):

@@ -84,10 +84,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
 // and joins the waves.  Units are 16 rows of a page at a multiple of 16, so that a unit lies in one page.
 //
 // Bound by the cache's rows from memory.  A wave has the next tile's K under way while it works on a tile, and the next V
-// from its end on; three workgroups of four waves share a CU (head_dim 128: 167 registers).  64 sequences of 17 - 8192
+// from its end on; three workgroups of four waves, or two of six, share a CU (head_dim 128: 167 registers).  64 sequences of 17 - 8192
 // tokens, 32 query and 8 KV heads of 128, bf16: 182 us for 1.08 GB, 5.9 TB/s (a plain streaming read: 6.7); one
 // of 131071: 92 us for 537 MB, 5.8 TB/s.  With little to read it is the chain of loads: 281 tokens, 32 heads,
-// 8.1 us, of which an empty kernel takes 2.0, the first tile with all that it waits for 2.9, two more 1.6 each.
+// 7.3 us, of which an empty kernel takes 2.0, the first tile with all that it waits for 3.3, the second 1.6.
 // 32-bit sums: queries and weights enter the bf16 products in three parts, which is all of their 24 bits.
 
 struct PagedAttnArgs {
@@ -318,14 +318,14 @@ struct PagedTile<float, DP, NT> {
   }
 };
 
-// One workgroup = (sequence, KV head, block of 16 query heads, split); its four waves take tiles in turn.  A lane of a
+// One workgroup = (sequence, KV head, block of 16 query heads, split); its waves (NW) take tiles in turn.  A lane of a
 // wave looks up the page of one of the wave's units, all of them before the first is needed: a split has at most
 // kBatchUnits of them per wave.  grid.x = sequences * KV heads * splits, rounded up to a multiple of 8, * blocks.
 constexpr int kBatchUnits = 64, kPagedWaves = 4;
-template <typename T, int DP, int NT>
-__global__ __launch_bounds__(64 * kPagedWaves, DP == 256 ? 1 : (DP == 128 && sizeof(T) == 4 ? 2 : 3)) void paged_attention_mfma(const PagedAttnArgs a) {
+template <typename T, int DP, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, DP == 256 ? 1 : (DP == 128 && sizeof(T) == 4 ? 2 : 3)) void paged_attention_mfma(const PagedAttnArgs a) {
   using Tile = PagedTile<T, DP, NT>;
-  constexpr int kU = Tile::kUnits, kPitch = DP + 4, NW = kPagedWaves;
+  constexpr int kU = Tile::kUnits, kPitch = DP + 4;
   __shared__ float s_m[NW][16], s_l[NW][16];
   // a wave's keys, and in their place its outputs when they are done with
   constexpr size_t kKeyBytes = (size_t)kU * 16 * DP * sizeof(T), kOutBytes = sizeof(float) * 16 * kPitch, kWaveBytes = kKeyBytes > kOutBytes ? kKeyBytes : kOutBytes;

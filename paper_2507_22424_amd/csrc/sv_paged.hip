@@ -28,35 +28,47 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   return (long long)c.n_seqs * n_q * (pieces > 1 ? pieces : 1) > (1ll << 23) ? SV_ERR_SHAPE : SV_OK;
 }
 
-// How a call is split over the chip, in workgroups' rounds (a tile for each of the four waves: 128 rows of a bf16
-// cache, 64 of a float32 one).  Up to one workgroup per CU a piece may be as short as a round, if there are three
-// pieces at least (the second launch, which joins them, takes 4 us): 600 tokens, 8 KV heads, 11.4 us in one piece, 9.3 in four.
-// Pieces of more than ten rounds are cut further, into pieces of four: until as many run as can at a time (three per CU),
-// or four times as many for several sequences, some of which are shorter than others (24 float32 sequences of up to 1500
-// tokens, 11.8 rounds: 17.7 us in two pieces, 15.2 in five; 64 of 17 - 8192 tokens: 214 us in 1024 pieces, 202 in three times as many; but 48 of
-// 1028 visible tokens, 8.3 rounds: 18.9 us in one, 21.5 in two, and 4 float32 ones of up to 3000, 18.1 us in eight, 24.0 in
-// eleven).  A piece has a unit of 16 rows at least for each query head of a KV head, beside whose rows its results would
-// not be little.  Splits (and with them the scratch) never get fewer as max_len grows.
+// How a call is split over the chip, in workgroups' rounds (a tile for each wave).  A workgroup has four waves, or six or
+// eight ("wide") where registers leave room for two of these on a CU, if that saves a round and there is a workgroup per CU
+// at most, or more than six rounds' work for each (32 and 8 heads of 128, bf16: 281 tokens 8.1 us narrow, 7.3 wide, 48
+// sequences of 1028 visible tokens 18.1, 16.4; but 48 of up to 300 tokens 12.6, 14.6, 100 tokens 5.3, 5.6).
+// Up to one workgroup per CU a row is cut into pieces of a round, if that saves three rounds (the second launch,
+// which joins them, takes 4 us), or two narrow ones, which take longer: 600 tokens, 10.0 us in one piece, 8.4 in four;
+// 16 sequences of up to 600, 10.9 in one, 11.6 in two; one of 300 and heads of 256, 12.5 in one, 10.0 in three.
+// Whole rows of more than ten wide rounds, and pieces of more than ten narrow ones, are cut further, into pieces of four:
+// until as many run as can at a time (three per CU), or four times as many for several sequences, some of which are shorter
+// than others (24 float32 sequences of up to 1500 tokens, 11.8 rounds: 17.7 us in two pieces, 15.0 in five; 64 of 17 - 8192 tokens:
+// 214 us in 1024 pieces, 202 in three times as many; but 32 of up to 1500, 7.8 rounds: 25.1 us whole, 27.4 in two, and 4
+// float32 ones of up to 3000, 18.1 us in eight, 24.0 in eleven).  A piece has a unit of 16 rows at least for each query
+// head of a KV head, beside whose rows its results would not be little.  Splits (and with them the scratch) never get
+// fewer as max_len grows.
 constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 4 * kGroupsOne;
 constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
-  int n_blocks, n_split, split_units;
+  int n_blocks, n_split, split_units, waves;
   size_t rows, part, part_ml, bytes;
 };
+static int wide_waves(const sv_paged_cache& c) {
+  return c.head_dim <= 64 ? 8 : (c.head_dim <= 128 && c.dtype == SV_BF16 ? 6 : kPagedWaves);
+}
 static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
   PagedPlan p;
   p.n_blocks = ceil_div(n_q / c.n_kv_heads, 16);
   const int tasks = c.n_seqs * c.n_kv_heads * p.n_blocks;        // (2^30 at most)
-  const int G = n_q / c.n_kv_heads, round = kPagedWaves * (c.dtype == SV_F32 ? 1 : 2);
-  auto pieces = [&](long long most, int least_units, int least_pieces) {
-    const int fill = n_units / (G > least_units ? G : least_units);
-    return fill < least_pieces ? 1 : (int)(fill < most ? fill : most);
-  };
-  p.n_split = pieces(kGroupsSmall / tasks, round, 3);
-  if (p.n_split < 1) p.n_split = 1;
-  const int cut = ceil_div(n_units, p.n_split) > 10 * round ? pieces(ceil_div(c.n_seqs > 1 ? kGroupsRagged : kGroupsOne, tasks), 4 * round, 2) : 1;
+  const int G = n_q / c.n_kv_heads, tile = c.dtype == SV_F32 ? 1 : 2, round = kPagedWaves * tile, wide = wide_waves(c) * tile;
+  int few = kGroupsSmall / tasks;
+  for (const int most : {ceil_div(n_units, wide), n_units / G}) few = most < few ? most : few;
+  const int saved = few > 1 ? ceil_div(n_units, wide) - ceil_div(n_units, few * wide) : 0;
+  p.n_split = saved >= (wide > round ? 3 : 2) ? few : 1;
+  int cut = 1;
+  if (ceil_div(n_units, p.n_split) > 10 * (p.n_split > 1 ? round : wide)) {
+    const int most = ceil_div(c.n_seqs > 1 ? kGroupsRagged : kGroupsOne, tasks), fill = n_units / (G > 4 * round ? G : 4 * round);
+    cut = fill < most ? fill : most;
+  }
   for (const int n : {cut, ceil_div(n_units, kPagedWaves * kBatchUnits)}) p.n_split = n > p.n_split ? n : p.n_split;
   p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
+  const bool room = tasks * p.n_split <= kGroupsSmall || p.split_units > 6 * round;
+  p.waves = room && ceil_div(p.split_units, wide) < ceil_div(p.split_units, round) ? wide_waves(c) : kPagedWaves;
   p.rows = (size_t)c.n_seqs * n_q;
   p.part = 0;
   p.part_ml = p.n_split > 1 ? align_up(p.rows * p.n_split * c.head_dim * 4, kAlign) : 0;
@@ -138,9 +150,17 @@ int sv_paged_attention(const sv_paged_cache* cache, const int32_t* seq_len, int 
   auto run = [&](auto t, auto past) {
     using T = decltype(t);
     constexpr int NT = decltype(past)::value;
-    if (cache->head_dim <= 64) paged_attention_mfma<T, 64, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
-    else if (cache->head_dim <= 128) paged_attention_mfma<T, 128, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
-    else paged_attention_mfma<T, 256, NT><<<groups, 64 * kPagedWaves, 0, st>>>(a);
+    auto launch = [&](auto dp, auto waves) {
+      paged_attention_mfma<T, decltype(dp)::value, NT, decltype(waves)::value><<<groups, 64 * decltype(waves)::value, 0, st>>>(a);
+    };
+    auto by_waves = [&](auto dp, auto most) {
+      if constexpr (NT == 0 && decltype(most)::value > kPagedWaves)
+        if (p.waves > kPagedWaves) return launch(dp, most);
+      launch(dp, std::integral_constant<int, kPagedWaves>{});
+    };
+    if (cache->head_dim <= 64) by_waves(std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
+    else if (cache->head_dim <= 128) by_waves(std::integral_constant<int, 128>{}, std::integral_constant<int, sizeof(T) == 2 ? 6 : kPagedWaves>{});
+    else by_waves(std::integral_constant<int, 256>{}, std::integral_constant<int, kPagedWaves>{});
   };
   auto typed = [&](auto past) {
     if (cache->dtype == SV_F32) run(0.f, past);

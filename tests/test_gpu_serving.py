@@ -479,6 +479,31 @@ def test_attention_split_over_the_length(dtype, nq, nkv, d, page, lens):
         say(f"[split {dtype} {nq}/{nkv} x {d} lengths {lens} window {window}] {worst:.1e}")
 
 
+@pytest.mark.parametrize("dtype,nq,nkv,d,page,lens,window,sink", [
+    ("bf16", 8, 2, 128, 16, [0, 1, 129, 191, 192, 193, 383, 384], 0, 0), ("bf16", 6, 2, 104, 32, [385, 500, 577, 600, 3], 0, 0),
+    ("bf16", 4, 1, 64, 16, [0, 1, 130, 256, 257, 500, 511, 512, 513], 0, 0), ("bf16", 4, 1, 64, 64, [1100, 700, 20], 0, 0),
+    ("f32", 4, 2, 48, 16, [0, 1, 65, 127, 128, 129, 250, 256, 300], 0, 0), ("f32", 16, 1, 64, 32, [900, 65, 64], 0, 0),
+    ("bf16", 8, 4, 64, 16, list(range(700, 961, 4)), 0, 0), ("bf16", 16, 8, 128, 16, list(range(690, 1100, 12)), 0, 0),
+    ("bf16", 16, 8, 128, 32, list(range(690, 1100, 12)), 900, 5), ("bf16", 4, 1, 64, 16, [3000, 1200, 490], 470, 20),
+    ("f32", 2, 1, 64, 16, [2000, 200, 7], 230, 4), ("bf16", 32, 1, 128, 16, [380, 200, 97], 0, 0)])
+def test_attention_of_workgroups_of_more_waves(dtype, nq, nkv, d, page, lens, window, sink):
+    """Rows of two rounds and more, whole and in pieces, over few workgroups and over many; a page outside the pool too."""
+    a = Attend(dtype, nq, nkv, d, page, lens)
+    a.call(window, sink)
+    a.check(window, sink)
+    if window == 0:
+        b = int(np.argmax(a.lens))
+        a.cache.block_table[b, int(a.lens[b] - 1) // page] = a.n_pages
+        a.call()
+        assert a.status.cpu().tolist() == [int(i == b) for i in range(len(lens))]
+        keep = a.table[b].copy()
+        a.table[b, int(a.lens[b] - 1) // page:] = -1
+        short = list(a.lens)
+        short[b] = int(a.lens[b] - 1) // page * page
+        a.check(lens=short, status=[int(i == b) for i in range(len(lens))])
+        a.table[b] = keep
+
+
 def test_attention_with_a_bound_above_the_lengths():
     """max_len is a bound: shorter sequences, lengths above it (clamped) and below zero."""
     a = Attend("bf16", 8, 2, 128, 16, [100, 2000, 1500, 700])

@@ -85,8 +85,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a) {
 //
 // Bound by the cache's rows from memory.  A wave has the next tile's K under way while it works on a tile, and the next V
 // from its end on; three workgroups of four waves, or two of six, share a CU (head_dim 128: 167 registers).  64 sequences of 17 - 8192
-// tokens, 32 query and 8 KV heads of 128, bf16: 182 us for 1.08 GB, 5.9 TB/s (a plain streaming read: 6.7); one
-// of 131071: 92 us for 537 MB, 5.8 TB/s.  With little to read it is the chain of loads: 281 tokens, 32 heads,
+// tokens, 32 query and 8 KV heads of 128, bf16: 181 us for 1.08 GB, 5.9 TB/s (a plain streaming read: 6.7); one
+// of 131071: 89 us for 537 MB, 6.0 TB/s.  With little to read it is the chain of loads: 281 tokens, 32 heads,
 // 7.3 us, of which an empty kernel takes 2.0, the first tile with all that it waits for 3.3, the second 1.6.
 // 32-bit sums: queries and weights enter the bf16 products in three parts, which is all of their 24 bits.
 

@@ -15,6 +15,21 @@ from . import binding as sv
 from .workload import VerifyConfig
 
 
+class StepGraph(torch.cuda.CUDAGraph):
+    """A step of a VerifyPass as a HIP graph: a replay is a step of that pass."""
+
+    def __new__(cls, *_):
+        return super().__new__(cls)
+
+    def __init__(self, owner: "VerifyPass", want_logits: bool):
+        super().__init__()
+        self.owner, self.want_logits = owner, want_logits
+
+    def replay(self) -> None:
+        super().replay()
+        self.owner.logits_current = self.want_logits
+
+
 class VerifyPass:
     def __init__(self, wc: VerifyConfig, prefix_len: Sequence[int], parent: np.ndarray,
                  full_vocab: bool = False, device: str = "cuda", extra_capacity: int = 0):
@@ -58,6 +73,10 @@ class VerifyPass:
         self.best_node = torch.zeros(self.B, dtype=torch.int32, device=device)
         self.path = torch.zeros(self.B, self.d_cap + 1, dtype=torch.int32, device=device)
         self.out_tokens = torch.zeros(self.B, self.d_cap + 1, dtype=torch.int32, device=device)
+        # whether the last pass wrote the logits of the present inputs; a recording other than capture_step()'s is
+        # replayed out of sight, so that from then on the caller is taken at their word
+        self.logits_current = False
+        self.logits_recorded = False
         self.probs: Optional[torch.Tensor] = None             # of accept_sampled(), with its status
         self.accept_status: Optional[torch.Tensor] = None
 
@@ -97,6 +116,7 @@ class VerifyPass:
     def set_hidden(self, x: torch.Tensor) -> None:
         """x: [B*T, H] in the storage dtype or float32; widened to the float32 stream."""
         self.x0.copy_(x.reshape(self.M, -1).to(torch.float32))
+        self.logits_current = False
 
     def set_draft(self, draft: np.ndarray) -> None:
         self.draft.copy_(torch.from_numpy(np.ascontiguousarray(draft, dtype=np.int32).reshape(-1)))
@@ -108,6 +128,7 @@ class VerifyPass:
         sv_verify_layer call per layer).  head:
         "packed" (sv_action_head_argmax_packed), "plain" (sv_action_head_argmax on the raw
         rows) or "auto" (packed where a packed head has been loaded)."""
+        self.logits_current = False
         self.x.copy_(self.x0)
         n = self.wc.n_layers if n_layers is None else n_layers
         views = [kv.struct for kv in self.kv[:n]]
@@ -130,6 +151,8 @@ class VerifyPass:
             sv.sv_action_head_argmax(self.cfg, self.g_final, self.w_lm, self.x, self.M,
                                      self.vocab_lo, self.vocab_hi, self.token,
                                      self.logits if want_logits else None, self.workspace)
+        self.logits_current = want_logits
+        self.logits_recorded |= want_logits and torch.cuda.is_current_stream_capturing()
 
     def accept(self, r: int, target: Optional[torch.Tensor] = None) -> None:
         sv.sv_relaxed_accept(self.tree.struct, self.draft, self.token if target is None else target,
@@ -140,9 +163,12 @@ class VerifyPass:
     def accept_sampled(self, u_accept: torch.Tensor, u_draw: torch.Tensor, temperature: float = 1.0,
                        draft_prob: Optional[torch.Tensor] = None) -> None:
         """Acceptance that keeps the verifier's distribution at this temperature, from the logits of the last
-        forward(want_logits=True) and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
+        pass and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
         [B*T, scored tokens] where the drafter drew its tokens.  Leaves what accept() leaves, so that
-        commit() follows; accept_status is not 0 where an episode had nothing to draw from."""
+        commit() follows; accept_status is not 0 where an episode had nothing to draw from.  Refuses where the last
+        pass left no logits (want_logits=False) or hidden rows, trees or prefixes have changed since."""
+        if not (self.logits_current or self.logits_recorded or torch.cuda.is_current_stream_capturing()):
+            raise RuntimeError("accept_sampled: no logits of the present inputs, run a pass with want_logits=True first")
         if self.probs is None:
             self.probs = torch.empty_like(self.logits)
             self.accept_status = torch.zeros(self.B, dtype=torch.int32, device=self.device)
@@ -168,14 +194,18 @@ class VerifyPass:
         with torch.cuda.stream(side):        # once outside the capture: nothing is set up lazily inside it
             self.step(r, want_logits, head)
         torch.cuda.current_stream().wait_stream(side)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            self.step(r, want_logits, head)
+        graph, recorded = StepGraph(self, want_logits), self.logits_recorded
+        try:
+            with torch.cuda.graph(graph):
+                self.step(r, want_logits, head)
+        finally:
+            self.logits_recorded = recorded  # (this graph tells when it is replayed)
         return graph
 
     def set_tree(self, parent: np.ndarray) -> None:
         """New draft trees (same B, T) for the next step."""
         self.tree = sv.DeviceTree(parent, self.B, self.T, self.d_cap, self.device)
+        self.logits_current = False
 
     def commit(self) -> None:
         """Make the accepted paths part of the prefix in every layer (outer loop of Alg. 1).
@@ -194,6 +224,7 @@ class VerifyPass:
                               self.B, self.d_cap)
         # all layers share the prefix lengths of layer 0's holder
         sv.sv_advance_prefix(self.kv[0].prefix_len, self.accepted_len, self.B, self.d_cap)
+        self.logits_current = False
         for l in range(self.wc.n_layers):
             self.kv[l].struct.prefix_len_max = self.kv[l].struct.prefix_len_max + advance
 

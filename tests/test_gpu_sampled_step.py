@@ -1,0 +1,68 @@
+"""Sampled acceptance as a step of VerifyPass on an MI355X: whose logits it reads, behind passes and replays."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_22424_amd import workload as wl
+from paper_2507_22424_amd.runner import VerifyPass
+
+from parity_utils import say
+
+pytestmark = pytest.mark.gpu
+
+B, T, V = 2, 6, 64
+PARENT = [-1, 0, 0, 1, 1, 2]
+
+
+def _pass():
+    cfg = wl.C2.scaled(name="bf16-sampled-step", index=63, n_layers=1, hidden=512, n_heads=4, head_dim=128, mlp_dim=1536, vocab=256,
+                       n_bins=V, n_episodes=B, tree_nodes=T, prefix_lo=20, prefix_hi=30, max_depth=2, max_children=2, spine_lo=2)
+    pl = wl.prefix_lengths(cfg)
+    vp = VerifyPass(cfg, pl, np.array(PARENT * B), extra_capacity=4 * T)
+    vp.load_layer(0, wl.layer_weights(cfg, 0))
+    for b in range(B):
+        vp.load_prefix(0, b, *wl.prefix_kv(cfg, b, 0, int(pl[b])))
+    head = wl.head_weights(cfg)
+    vp.load_head(head["g_final"], head["w_lm"])
+    return vp
+
+
+def _inputs(vp, seed):
+    gen = torch.Generator().manual_seed(seed)
+    hidden = 0.5 * torch.randn(B * T, vp.wc.hidden, generator=gen)
+    draft = vp.wc.vocab - V + torch.randint(0, V, (B * T,), generator=gen)
+    return hidden, draft.numpy(), torch.rand(B * T, generator=gen).cuda(), torch.rand(B, generator=gen).cuda()
+
+
+def _outputs(vp):
+    return [t.clone() for t in (vp.probs, vp.accept_mask, vp.accepted_len, vp.best_node, vp.path, vp.out_tokens, vp.accept_status)]
+
+
+def test_sampling_reads_the_logits_of_the_last_pass_or_refuses():
+    """Eager passes and replays of recorded steps, with logits and without, in turn."""
+    vp = _pass()
+    hidden, draft, ua, ud = _inputs(vp, 0)
+    vp.set_hidden(hidden)
+    vp.set_draft(draft)
+    with_logits, without = vp.capture_step(4, want_logits=True), vp.capture_step(4)
+    with pytest.raises(RuntimeError, match="no logits"):
+        vp.accept_sampled(ua, ud)
+    for rep in range(3):
+        say(f"[sampled step] replay {rep}")
+        hidden, draft, ua, ud = _inputs(vp, 1 + rep)
+        vp.set_hidden(hidden)
+        vp.set_draft(draft)
+        vp.forward()
+        vp.accept_sampled(ua, ud, 0.8)
+        want = _outputs(vp)
+        assert bool((vp.probs.sum(1) - 1).abs().max() < 1e-5)
+        vp.set_hidden(hidden)
+        vp.logits.fill_(3.0)
+        with pytest.raises(RuntimeError, match="no logits"):
+            vp.accept_sampled(ua, ud, 0.8)
+        without.replay()
+        with pytest.raises(RuntimeError, match="no logits"):
+            vp.accept_sampled(ua, ud, 0.8)
+        with_logits.replay()
+        vp.accept_sampled(ua, ud, 0.8)
+        assert all(torch.equal(x, y) for x, y in zip(want, _outputs(vp)))

@@ -77,8 +77,8 @@ class VerifyPass:
         # replayed out of sight, so that from then on the caller is taken at their word
         self.logits_current = False
         self.logits_recorded = False
-        self.probs: Optional[torch.Tensor] = None             # of accept_sampled(), with its status
-        self.accept_status: Optional[torch.Tensor] = None
+        self.probs = torch.zeros_like(self.logits)            # of accept_sampled(), with its status
+        self.accept_status = torch.zeros(self.B, dtype=torch.int32, device=device)
 
     # ---- loading -------------------------------------------------------------------
     def load_layer(self, layer: int, raw: Dict[str, torch.Tensor]) -> None:
@@ -166,12 +166,10 @@ class VerifyPass:
         pass and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
         [B*T, scored tokens] where the drafter drew its tokens.  Leaves what accept() leaves, so that
         commit() follows; accept_status is not 0 where an episode had nothing to draw from.  Refuses where the last
-        pass left no logits (want_logits=False) or hidden rows, trees or prefixes have changed since."""
+        pass left no logits (want_logits=False) or hidden rows, trees or prefixes have changed since.  Allocates nothing, so that it
+        can be recorded behind a recorded forward(); a recording keeps u_accept, u_draw, draft_prob and the temperature."""
         if not (self.logits_current or self.logits_recorded or torch.cuda.is_current_stream_capturing()):
             raise RuntimeError("accept_sampled: no logits of the present inputs, run a pass with want_logits=True first")
-        if self.probs is None:
-            self.probs = torch.empty_like(self.logits)
-            self.accept_status = torch.zeros(self.B, dtype=torch.int32, device=self.device)
         sv.sv_token_probs(self.logits, temperature, self.probs)
         sv.sv_sampled_accept(self.tree.struct, self.draft, self.probs, draft_prob, self.vocab_lo, u_accept, u_draw,
                              self.B, self.d_cap, self.accept_mask, self.accepted_len, self.best_node, self.path,

@@ -66,3 +66,39 @@ def test_sampling_reads_the_logits_of_the_last_pass_or_refuses():
         with_logits.replay()
         vp.accept_sampled(ua, ud, 0.8)
         assert all(torch.equal(x, y) for x, y in zip(want, _outputs(vp)))
+
+
+def test_a_recorded_sampled_step_follows_its_inputs():
+    """Pass and sampled acceptance in one graph, their first calls of all inside it but for the pass's; replayed with new
+    inputs, eager steps between."""
+    vp = _pass()
+    hidden, draft, ua, ud = _inputs(vp, 0)
+    vp.set_hidden(hidden)
+    vp.set_draft(draft)
+    vp.forward()
+    held = torch.cuda.memory_allocated()
+    vp.accept_sampled(ua, ud, 0.8)
+    assert torch.cuda.memory_allocated() == held
+    vp = _pass()
+    vp.set_hidden(hidden)
+    vp.forward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vp.forward()
+        vp.accept_sampled(ua, ud, 0.8)
+    for rep in range(4):
+        hidden, draft, a, d = _inputs(vp, 10 + rep)
+        ua.copy_(a)
+        ud.copy_(d)
+        vp.set_hidden(hidden)
+        vp.set_draft(draft)
+        vp.forward()
+        vp.accept_sampled(a, d, 0.8)
+        want = _outputs(vp)
+        for t in (vp.logits, vp.probs, vp.path, vp.out_tokens, vp.accepted_len, vp.accept_mask):
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, _outputs(vp)))

@@ -90,3 +90,12 @@ def test_recorded_passes_are_not_refused(vp, calls):
     calls.capturing = False
     vp.set_hidden(torch.zeros(8, 512))               # (and a replay)
     _sample(vp)
+
+
+def test_sampling_allocates_nothing(vp):
+    """Its buffers are the object's from the beginning: a first call may be one that is recorded."""
+    held = [t.data_ptr() for t in (vp.probs, vp.accept_status)]
+    assert vp.probs.shape == vp.logits.shape and vp.accept_status.shape == (2,)
+    vp.forward()
+    _sample(vp)
+    assert held == [t.data_ptr() for t in (vp.probs, vp.accept_status)]

@@ -28,6 +28,7 @@ class StepGraph(torch.cuda.CUDAGraph):
     def replay(self) -> None:
         super().replay()
         self.owner.logits_current = self.want_logits
+        self.owner.clear_accept_status()     # (the recording may be older than the first sampled acceptance)
 
 
 class VerifyPass:
@@ -79,6 +80,7 @@ class VerifyPass:
         self.logits_recorded = False
         self.probs = torch.zeros_like(self.logits)            # of accept_sampled(), with its status
         self.accept_status = torch.zeros(self.B, dtype=torch.int32, device=device)
+        self.samples = False                                  # from the first accept_sampled() on
 
     # ---- loading -------------------------------------------------------------------
     def load_layer(self, layer: int, raw: Dict[str, torch.Tensor]) -> None:
@@ -159,17 +161,25 @@ class VerifyPass:
                              self.wc.action_lo, self.wc.n_bins, r, self.B, self.d_cap,
                              self.accept_mask, self.accepted_len, self.best_node, self.path,
                              self.out_tokens)
+        self.clear_accept_status()
+
+    def clear_accept_status(self) -> None:
+        """What is accepted was not sampled: accept_status is that of an earlier acceptance, if any."""
+        if self.samples:
+            self.accept_status.zero_()
 
     def accept_sampled(self, u_accept: torch.Tensor, u_draw: torch.Tensor, temperature: float = 1.0,
                        draft_prob: Optional[torch.Tensor] = None) -> None:
         """Acceptance that keeps the verifier's distribution at this temperature, from the logits of the last
         pass and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
         [B*T, scored tokens] where the drafter drew its tokens.  Leaves what accept() leaves, so that
-        commit() follows; accept_status is not 0 where an episode had nothing to draw from.  Refuses where the last
+        commit() follows; accept_status is not 0 where an episode had nothing to draw from, and commit() refuses
+        where nothing but NaN or masked logits were there (bit 1).  Refuses where the last
         pass left no logits (want_logits=False) or hidden rows, trees or prefixes have changed since.  Allocates nothing, so that it
         can be recorded behind a recorded forward(); a recording keeps u_accept, u_draw, draft_prob and the temperature."""
         if not (self.logits_current or self.logits_recorded or torch.cuda.is_current_stream_capturing()):
             raise RuntimeError("accept_sampled: no logits of the present inputs, run a pass with want_logits=True first")
+        self.samples = True
         sv.sv_token_probs(self.logits, temperature, self.probs)
         sv.sv_sampled_accept(self.tree.struct, self.draft, self.probs, draft_prob, self.vocab_lo, u_accept, u_draw,
                              self.B, self.d_cap, self.accept_mask, self.accepted_len, self.best_node, self.path,
@@ -207,11 +217,14 @@ class VerifyPass:
 
     def commit(self) -> None:
         """Make the accepted paths part of the prefix in every layer (outer loop of Alg. 1).
-        Refuses when the last pass raised the status word (its results are then undefined) or
-        when the cache has no room left for another tree behind the longest possible prefix."""
+        Refuses when the last pass raised the status word (its results are then undefined), when a sampled
+        acceptance had no distribution to draw an episode's last token from (accept_status, bit 1), or when the cache has no room left for another tree behind the longest possible prefix."""
         st = self.placement_status()
         if st != 0:
             raise RuntimeError(f"verification pass raised status {st}: results undefined, nothing committed")
+        undrawn = torch.nonzero(self.accept_status & 2).flatten().tolist() if self.samples else []
+        if undrawn:
+            raise RuntimeError(f"sampled acceptance: no probability to draw from in episodes {undrawn}, nothing committed")
         # (the status read above has synchronised: the accepted lengths are on hand)
         advance = int(self.accepted_len.max().item()) + 1
         if self.kv[0].struct.prefix_len_max + advance > self.capacity - self.T:

@@ -102,3 +102,27 @@ def test_a_recorded_sampled_step_follows_its_inputs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(want, _outputs(vp)))
+
+
+def test_commit_refuses_rows_without_a_distribution():
+    """Logits of an episode that are all masked, or NaN: accept_status says so, and nothing is committed - until another
+    acceptance, sampled or not, eager or recorded, takes its place."""
+    vp = _pass()
+    hidden, draft, ua, ud = _inputs(vp, 0)
+    vp.set_hidden(hidden)
+    vp.set_draft(draft)
+    graph = vp.capture_step(4, want_logits=True)     # older than the first sampled acceptance
+    for bad in (float("nan"), -float("inf")):
+        for again in (graph.replay, lambda: vp.accept(4), lambda: (vp.forward(), vp.accept_sampled(ua, ud))):
+            vp.forward()
+            vp.logits[T:] = bad
+            vp.accept_sampled(ua, ud)
+            assert vp.accept_status.tolist() == [0, 3]
+            prefix, bound = vp.kv[0].prefix_len.clone(), vp.kv[0].struct.prefix_len_max
+            with pytest.raises(RuntimeError, match="episodes .1."):
+                vp.commit()
+            assert torch.equal(vp.kv[0].prefix_len, prefix) and vp.kv[0].struct.prefix_len_max == bound
+            again()
+            assert vp.accept_status.tolist() == [0, 0]
+    vp.commit()
+    assert torch.equal(vp.kv[0].prefix_len, prefix + vp.accepted_len + 1)

@@ -26,7 +26,7 @@ class _Calls:
     def _made(self, name, args):
         self.made.append(name)
         if name == "sv_sampled_accept":
-            args[-1].fill_(self.status)
+            args[-1].copy_(torch.as_tensor(self.status))
 
 
 @pytest.fixture
@@ -99,3 +99,18 @@ def test_sampling_allocates_nothing(vp):
     vp.forward()
     _sample(vp)
     assert held == [t.data_ptr() for t in (vp.probs, vp.accept_status)]
+
+
+def test_commit_refuses_an_episode_that_had_nothing_to_draw_from(vp, calls):
+    for status, refused in ((0, False), (1, False), (3, True)):          # (1: drawn from the target's row itself)
+        vp.forward()
+        calls.status = torch.tensor([0, status], dtype=torch.int32)
+        vp.accept_sampled(torch.zeros(8), torch.zeros(2))
+        calls.made.clear()
+        if refused:
+            with pytest.raises(RuntimeError, match=r"episodes \[1\]"):
+                vp.commit()
+            assert not calls.made
+            vp.accept(4)                             # what is accepted now was not sampled
+        vp.commit()
+        assert calls.made[-1] == "sv_advance_prefix"

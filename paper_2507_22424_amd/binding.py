@@ -489,7 +489,7 @@ def sv_sampled_accept(tree: Tree, draft_token: torch.Tensor, target_prob: torch.
                       out_tokens: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """target_prob, draft_prob: [B*T, columns]; the other sizes as in sv_relaxed_accept."""
     n, n_vocab = B * tree.n_nodes, target_prob.shape[-1]
-    if max(n_vocab, abs(vocab_lo), d_cap) > _I32_MAX or target_prob.numel() != n * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
+    if max(n_vocab, abs(vocab_lo), B, d_cap) > _I32_MAX or target_prob.numel() != n * n_vocab or (draft_prob is not None and draft_prob.shape != target_prob.shape) or \
             draft_token.numel() != n or u_accept.numel() != n or u_draw.numel() != B or accept_mask.numel() != n or \
             accepted_len.numel() != B or best_node.numel() != B or status.numel() != B or \
             path.numel() != B * (d_cap + 1) or out_tokens.numel() != B * (d_cap + 1):
@@ -519,12 +519,15 @@ def sv_paged_append(cache: "PagedCache", token_seq: torch.Tensor, token_pos: tor
                     k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor], rope_theta: float,
                     status: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, k, v: [tokens, heads, head_dim] float32, views of a fused projection among them."""
-    n, c, dev = token_seq.numel(), cache.struct, _device()
+    n, c = token_seq.numel(), cache.struct
     nkv, d = c.n_kv_heads, c.head_dim
     if token_pos.numel() != n or (status is not None and status.numel() != n) or (q is None) != (q_out is None) or \
             (q is not None and (q.dim() != 3 or q_out.shape != q.shape)):
         raise ValueError("paged_append: tensor sizes do not match the tokens")
     nq = 0 if q is None else q.shape[1]
+    if max(n, nq) > _I32_MAX:
+        raise ValueError("paged_append: tokens and query heads must be 32-bit numbers")
+    dev = _device()
     qp, q_stride = (None, 0) if q is None else _token_rows(q, n, nq, d, dev, "q")
     kp, k_stride = _token_rows(k, n, nkv, d, dev, "k")
     vp, v_stride = _token_rows(v, n, nkv, d, dev, "v")
@@ -554,8 +557,8 @@ def sv_paged_attention(cache: "PagedCache", seq_len: torch.Tensor, max_len: int,
             seq_len.numel() != n_seqs or (lse is not None and lse.numel() != n_seqs * q.shape[1]) or \
             (status is not None and status.numel() != n_seqs):
         raise ValueError("paged_attention: tensor sizes do not match the cache")
-    if not -_I32_MAX <= min(max_len, window, n_sink) <= max(max_len, window, n_sink) <= _I32_MAX:
-        raise ValueError("paged_attention: max_len, window and n_sink must be 32-bit numbers")
+    if not -_I32_MAX <= min(max_len, window, n_sink) <= max(max_len, window, n_sink, q.shape[1]) <= _I32_MAX:
+        raise ValueError("paged_attention: max_len, window, n_sink and query heads must be 32-bit numbers")
     dev = _device()
     cache.check_device(dev)
     rc = lib().sv_paged_attention(
@@ -605,6 +608,8 @@ class PagedCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor):
         if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or block_table.dim() != 2:
             raise ValueError("k and v must be [n_pages, n_kv_heads, page_size, head_dim], block_table [n_seqs, max_pages]")
+        if max(*k.shape, *block_table.shape) > _I32_MAX:
+            raise ValueError("a paged cache's sizes must be 32-bit numbers")
         if k.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"a paged cache holds float32 or bfloat16, got {k.dtype}")
         if k.device != v.device or k.device != block_table.device:

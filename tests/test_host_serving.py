@@ -142,3 +142,26 @@ def test_numbers_past_32_bits_are_refused():
     for p, lo in ((torch.zeros(1, 1).expand(2, big + 1), 0), (torch.zeros(2, 5), big), (torch.zeros(2, 5), -big)):
         with pytest.raises(ValueError, match="sizes"):
             sv.sv_sampled_accept(tree, nodes.int(), p, None, lo, nodes, nodes[:1], 1, 7, nodes.byte(), out[:1], out[:1], out, out, out[:1])
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Sizes of tensors too: a page of 2^32 + 16 rows is none of 16."""
+    big = 1 << 32
+    page, table = torch.zeros(1, 1, 16, 8), torch.zeros(1, 1, dtype=torch.int32)
+    for k, t in ((page.expand(big + 1, 1, 16, 8), table), (page.expand(1, big + 1, 16, 8), table),
+                 (page[:, :, :1].expand(1, 1, big + 16, 8), table), (page[..., :1].expand(1, 1, 16, big + 8), table),
+                 (page, table.expand(big + 1, 1)), (page, table.expand(1, big + 1))):
+        with pytest.raises(ValueError, match="32-bit"):
+            sv.PagedCache(k, k, t)
+    cache = type("Cache", (), {"struct": _view(n_seqs=1, n_kv_heads=1, head_dim=8, max_pages=4)})()
+    ids, x, ws = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, 8), torch.zeros(256, dtype=torch.uint8)
+    many, heads = x.expand(big + 1, 1, 8), x.expand(1, big + 1, 8)
+    with pytest.raises(ValueError, match="32-bit"):
+        sv.sv_paged_append(cache, ids.expand(big + 1), ids.expand(big + 1), None, many, many, None, 1e4)
+    with pytest.raises(ValueError, match="32-bit"):
+        sv.sv_paged_append(cache, ids, ids, heads, x, x, heads, 1e4)
+    with pytest.raises(ValueError, match="32-bit"):
+        sv.sv_paged_attention(cache, ids, 5, heads, 0.1, 0, 0, heads, None, None, ws)
+    tree, f, i, m = sv.Tree(4096, 4096, 4096, 1, 1), torch.zeros(1).expand(big + 1), ids.expand(big + 1), ws[:1].expand(big + 1)
+    with pytest.raises(ValueError, match="sizes"):
+        sv.sv_sampled_accept(tree, i, f[:, None], None, 0, f, f, big + 1, 0, m, i, i, i, i, i)

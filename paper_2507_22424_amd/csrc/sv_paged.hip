@@ -22,8 +22,9 @@ static PagedCache view(const sv_paged_cache& c) {
 
 static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
   if (n_q < 1 || n_q > (1 << 15) || n_q % c.n_kv_heads || max_len < 0 || max_len > c.max_pages * c.page_size) return SV_ERR_SHAPE;
-  // a launch has less than 2^32 threads: 256 for a piece of a row at most, which has 4096 rows of the cache at least where
-  // there are many, and 64 x 32 for a row that is joined from more than eight
+  // A launch has less than 2^32 threads.  Attention: up to 2^23 pieces (beyond some 3000 workgroups nothing is cut finer than
+  // 4096 rows) of 256 threads, of up to 512 where there are no more than kGroupsWide.  Join: 64 threads at most for a query
+  // head, 2048 for one of more than 16 pieces, which here means 3000 heads at most, or 65536 rows and up to 2^19 heads.
   const long long pieces = (max_len + 4095ll) / 4096;
   return (long long)c.n_seqs * n_q * (pieces > 1 ? pieces : 1) > (1ll << 23) ? SV_ERR_SHAPE : SV_OK;
 }
@@ -43,6 +44,7 @@ static int check_heads(const sv_paged_cache& c, int n_q, int max_len) {
 // head of a KV head, beside whose rows its results would not be little.  Splits (and with them the scratch) never get
 // fewer as max_len grows.
 constexpr int kGroupsSmall = 256, kGroupsOne = 768, kGroupsRagged = 4 * kGroupsOne;
+constexpr int kGroupsWide = 1 << 21;         // at most, of more than four waves: check_heads
 constexpr long long kInfinityCache = 256ll << 20;
 struct PagedPlan {
   int n_blocks, n_split, split_units, waves;
@@ -54,7 +56,7 @@ static int wide_waves(const sv_paged_cache& c) {
 static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
   PagedPlan p;
   p.n_blocks = ceil_div(n_q / c.n_kv_heads, 16);
-  const int tasks = c.n_seqs * c.n_kv_heads * p.n_blocks;        // (2^30 at most)
+  const int tasks = c.n_seqs * c.n_kv_heads * p.n_blocks;        // (2^23 at most)
   const int G = n_q / c.n_kv_heads, tile = c.dtype == SV_F32 ? 1 : 2, round = kPagedWaves * tile, wide = wide_waves(c) * tile;
   int few = kGroupsSmall / tasks;
   for (const int most : {ceil_div(n_units, wide), n_units / G}) few = most < few ? most : few;
@@ -67,7 +69,8 @@ static PagedPlan plan_paged(const sv_paged_cache& c, int n_q, int n_units) {
   }
   for (const int n : {cut, ceil_div(n_units, kPagedWaves * kBatchUnits)}) p.n_split = n > p.n_split ? n : p.n_split;
   p.split_units = (ceil_div(n_units < 1 ? 1 : n_units, p.n_split) + 1) / 2 * 2;
-  const bool room = tasks * p.n_split <= kGroupsSmall || p.split_units > 6 * round;
+  const int groups = tasks * p.n_split;
+  const bool room = groups <= kGroupsSmall || (p.split_units > 6 * round && groups <= kGroupsWide);
   p.waves = room && ceil_div(p.split_units, wide) < ceil_div(p.split_units, round) ? wide_waves(c) : kPagedWaves;
   p.rows = (size_t)c.n_seqs * n_q;
   p.part = 0;

@@ -799,3 +799,73 @@ def test_token_probs_of_long_rows_in_shares(rows):
     _check_probs(f64(p.cpu()), f64(z), float(np.float32(0.9)))
     sv.sv_token_probs(d, 0.9, d)
     assert torch.equal(d, p)
+
+
+# ---- forms and borders that the sizes above do not reach -------------------------------------------
+
+@pytest.mark.parametrize("rows", [1, 5])
+@pytest.mark.parametrize("n", [8192, 8193, 32768, 32769])
+def test_token_probs_where_the_kernel_changes(rows, n):
+    """The last column of a thread's registers, and the first that they do not hold."""
+    test_token_probs(rows, n)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("V", [40, 300, 5000, 20000, 40000])
+def test_rows_off_the_walk_have_no_effect(V, drawn):
+    """Rows of nodes that the walk did not come to hold NaN, infinity or mass everywhere: the same outputs."""
+    rng = np.random.default_rng(V)
+    B, T = 4, 20
+    a = Accept(_trees(B, T, 5, 3, rng), 5)
+    p, q = _probs(rng, (B, T, V), 1.0), _probs(rng, (B, T, V), 1.0) * 0.3 + _probs(rng, (B, T, V), 1.0) * np.float32(0.7)
+    tok = _draft_tokens(a.parents, p.astype(float), rng, drawn)
+    p, q = (torch.from_numpy(x.astype(np.float32)).cuda() for x in (p, q))
+    tok = torch.from_numpy(tok.reshape(-1)).int().cuda()
+    u, ud = torch.from_numpy(0.2 * rng.random(B * T)).float().cuda(), torch.from_numpy(rng.random(B)).float().cuda()
+    call = lambda: a.call(tok, p.view(B * T, V), q.view(B * T, V) if drawn else None, 0, u, ud)
+    keep = p.clone(), q.clone()
+    for first in (False, True):                      # by these numbers, and down to a leaf by each node's first child
+        if first:
+            u.zero_()
+        p.copy_(keep[0])
+        q.copy_(keep[1])
+        call()
+        want = [t.clone() for t in a.outputs()]
+        on = a.mask.view(B, T).bool()
+        assert bool((on.sum(1) < T).all()) and (not first or int(a.length.min()) > 0)
+        for junk in (float("nan"), float("inf"), 1e30, -1.0):
+            p[~on] = junk
+            q[~on] = junk
+            call()
+            assert all(torch.equal(x, y) for x, y in zip(want, a.outputs()))
+
+
+MANY = [i * 7 % 40 for i in range(60)] + [1290, 800, 500, 1000, 64]
+
+
+# more rows planned (sequences x units that max_len and the window allow) than the Infinity Cache holds: loads past the caches
+@pytest.mark.parametrize("dtype,nq,nkv,d,page,lens,max_len,window,sink", [
+    ("bf16", 8, 4, 64, 16, [0, 1, 17, 300, 1700, 2500], 90000, 0, 0), ("f32", 4, 4, 48, 32, [2500, 0, 129, 600], 90000, 0, 0),
+    ("bf16", 32, 8, 128, 64, [1, 700, 0, 3000], 60000, 0, 0), ("f32", 6, 2, 96, 16, [33, 1900, 5], 120000, 0, 0),
+    ("bf16", 16, 1, 256, 16, [2100, 40], 140000, 0, 0), ("f32", 3, 3, 192, 48, [15, 1000, 2000], 60000, 0, 0),
+    # whole rows, of which a workgroup has more rounds than it would take more waves for
+    ("bf16", 16, 16, 64, 16, MANY, 1290, 0, 0), ("bf16", 16, 16, 128, 32, MANY, 1290, 0, 0),
+    ("f32", 16, 16, 64, 16, MANY, 1290, 0, 0),
+    # a window, of rows in pieces and whole
+    ("bf16", 6, 2, 128, 16, [0, 3000, 900, 2000, 1], 100000, 99000, 5), ("bf16", 16, 16, 128, 16, MANY, 2000, 650, 20),
+    ("f32", 32, 16, 64, 16, MANY, 2000, 600, 33), ("f32", 16, 16, 256, 16, [n % 700 for n in MANY], 900, 530, 4)])
+def test_attention_past_the_caches(dtype, nq, nkv, d, page, lens, max_len, window, sink):
+    """Every type and size of head; with a page outside the pool too."""
+    units = -(-max_len // 16)
+    if window:
+        units = min(units, -(-sink // 16) + -(-window // 16) + 1)
+    assert len(lens) * units * 16 * 2 * nkv * d * (4 if dtype == "f32" else 2) > 256 << 20 and nq // nkv <= 16
+    a = Attend(dtype, nq, nkv, d, page, lens, max_len=max_len)
+    a.call(window, sink)
+    worst = a.check(window, sink)
+    say(f"[past the caches {dtype} {nq}/{nkv} x {d} max_len {max_len} window {window}] {worst:.1e}")
+    b = int(np.argmax(a.lens))
+    a.table[b, int(a.lens[b] - 1) // page] = a.n_pages
+    a.cache.block_table.copy_(torch.from_numpy(a.table))
+    a.call(window, sink)
+    a.check(window, sink, status=[int(i == b) for i in range(len(lens))])

@@ -123,7 +123,7 @@ struct VisibleRows {
   __device__ bool full(int unit) const {
     return unit * 16 + 16 <= len && (unit * 16 >= first || unit * 16 + 16 <= n_sink);
   }
-  // (without a branch: with one, the compiler left scores of rows in front of a window as they were)
+  // (joined bit by bit: with && and || each of a tile's rows takes a branch of its own)
   __device__ bool sees(int j) const { return (j < len) & ((j >= first) | (j < n_sink)); }
 };
 

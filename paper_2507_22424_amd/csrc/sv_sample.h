@@ -41,6 +41,8 @@ __device__ inline void store_prob(float* p, float v) {
 // dealt to gridDim.y workgroups, each of which goes through the whole row for the sum (a CU fetches some 50 bytes a
 // nanosecond: 3 rows of 128000 columns 25.3 us by one workgroup each, 14.8 by eight) - not in place, where one would
 // overwrite what another has still to read.
+// The exponent is (z - max) c with c = log2(e) / temperature rounded once, the quotient a product with the sum's rounded
+// reciprocal: 2^-24 of x more for an exponent x, half a step more for a quotient, than two divisions for each column.
 template <int NT, int K>
 __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, float c, float* p) {
   __shared__ float red[NT / 64];
@@ -111,12 +113,14 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
 // registers, two a lane, and goes through the walk for itself: children are found by ballot, a child's numbers come
 // by readlane, and the branches are uniform over the workgroup.  Only sums over whole rows (before a second
 // sibling, and for the draw) read the rows.
-// Sums are float64: the inputs are float32, so that a sum is exact unless its terms span more
-// than 2^29, and the choice of a token does not hang on the order of the summation.  They go from lane to lane by
-// data-parallel primitives (through LDS, and with every wave adding up all waves' parts by itself, 16 trees over
-// 4000 columns took 26.6 us, now 11.7).  Bound by what one CU fetches, some 50 - 60 bytes a nanosecond: 128 chains over
-// 128259 columns 33 us for 131 MB, where 20 would be the memory's time.  A tree over 256 columns, 5.3 us, is a chain of
-// loads: tree, probabilities of the tokens, the last row.
+// Sums are float64, in an order that the length of a row fixes: results are the same in every run.  They are not exact: p - less q is
+// rounded from a node's second refusal on, and a sum where range and number of its terms take more than 29 bits together.
+// They go from lane to lane by data-parallel primitives (through LDS, and with every wave adding up all waves' parts by
+// itself, 16 trees over 4000 columns, about four children to a node, took 26.6 us, 11.6 this way, 9.7 with rows held).
+// Bound for long rows by one CU per tree: chains of two nodes over 33000 - 256000 columns, of which p and q of one row are summed,
+// take 9 us and the row's bytes, 42 a nanosecond from memory (128 chains: 5.3 TB/s together) or 53 (32 chains), 45 and 68 from the
+// Infinity Cache; 128 over 128259 columns 33 us for 131 MB, where 20 would be the memory's time.  A tree over 256 columns,
+// 5.3 us, is a chain of loads: tree, probabilities of the tokens, the last row.
 
 struct SampleArgs {
   const int32_t* parent;
@@ -187,8 +191,9 @@ __device__ inline void rest_at(const RestOfRow& row, int i, int end, double* v) 
 }
 
 // A row that its workgroup holds from one sum to the next: a thread's columns of p in registers, those of q in LDS, which
-// no other thread reads (both in registers spills).  16 trees of 60 drawn tokens over 1000 / 4000 / 16000 / 32000 columns: 9.9 / 11.7 /
-// 17.8 / 28.9 us with each sum from the caches, 7.8 / 9.9 / 14.3 / 24.5 this way.
+// no other thread reads (both in registers spills).  16 trees of 60 drawn tokens over 1000 / 4000 / 16000 / 32000 columns, about
+// three children to a node: 9.4 / 10.7 / 14.8 / 21.0 us with each sum from the caches, 7.7 / 9.3 / 13.4 / 18.1 this way;
+// about four, which is more sums: 9.8 / 11.6 / 17.8 / 28.7 and 7.8 / 9.7 / 14.3 / 24.3.
 template <int NT>
 struct HeldRow {
   static constexpr int kColumns = NT == 64 ? 4 : (NT == 128 ? 8 : (NT == 256 ? 16 : 32));    // (each NT's longest row)

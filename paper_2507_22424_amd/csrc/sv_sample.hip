@@ -26,8 +26,8 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
 }
 
 static int sampled_accept(const SampleArgs& a, int B, hipStream_t st) {
-  // Threads by the length of a row (16 trees of 60 drawn tokens, us with 64 / 128 / 256 / 512 / 1024: 200 columns 6.1 / 6.9, 1000
-  // - / 7.8 / 8.4, 2000 - / 9.1 / 7.7, 4000 - / - / 9.9 / 12.3, 8000 - / - / 14.4 / 12.3, 16000 - / - / - / 14.3 / 15.0; not held: 128 chains
+  // Threads by the length of a row (16 trees of 60 drawn tokens, about four children to a node, us with 64 / 128 / 256 / 512 /
+  // 1024: 200 columns 6.1 / 6.9, 1000 - / 7.8 / 8.4, 2000 - / 9.1 / 7.7, 4000 - / - / 9.9 / 12.3, 8000 - / - / 14.4 / 12.3, 16000 - / - / - / 14.3 / 15.0; not held: 128 chains
   // of 128259 - / - / 56.0 / 32.9 / 32.1).  One wave takes 256 columns at most, see RowSearch::find.
   // Rows held take 128 KB of LDS for 1024 threads, so that one workgroup is on a CU instead of two: 400 trees of 32000
   // columns 57 us unheld, 42 held, but 1000 of 20000 78 and 86, 1000 chains 54 and 64.

@@ -174,9 +174,10 @@ class VerifyPass:
         pass and given random numbers (u_accept [B*T], u_draw [B]); draft_prob
         [B*T, scored tokens] where the drafter drew its tokens.  Leaves what accept() leaves, so that
         commit() follows; accept_status is not 0 where an episode had nothing to draw from, and commit() refuses
-        where nothing but NaN or masked logits were there (bit 1).  Refuses where the last
-        pass left no logits (want_logits=False) or hidden rows, trees or prefixes have changed since.  Allocates nothing, so that it
-        can be recorded behind a recorded forward(); a recording keeps u_accept, u_draw, draft_prob and the temperature."""
+        where nothing but NaN or masked logits were there (bit 1).  Refuses where the last pass left no logits
+        (want_logits=False), or after set_hidden(), set_tree() or commit() until the next pass.  Allocates nothing,
+        so that it can be recorded behind a recorded forward(); a recording keeps u_accept, u_draw, draft_prob and
+        the temperature."""
         if not (self.logits_current or self.logits_recorded or torch.cuda.is_current_stream_capturing()):
             raise RuntimeError("accept_sampled: no logits of the present inputs, run a pass with want_logits=True first")
         self.samples = True

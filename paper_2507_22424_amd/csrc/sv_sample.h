@@ -36,24 +36,29 @@ __device__ inline void store_prob(float* p, float v) {
   else *p = v;
 }
 
+constexpr float kProbsUnit = 0x1p-24f;
+
 // grid = (rows, 1 or shares of a row), block = NT.  A row of up to NT * K columns stays in registers, K of them per thread, and is read once;
 // a longer one (K = 0) is read twice, first for a running maximum and the sum that goes with it.  Its quotients can be
 // dealt to gridDim.y workgroups, each of which goes through the whole row for the sum (a CU fetches some 50 bytes a
 // nanosecond: 3 rows of 128000 columns 25.3 us by one workgroup each, 14.8 by eight) - not in place, where one would
 // overwrite what another has still to read.
-// The exponent is (z - max) c with c = log2(e) / temperature rounded once, the quotient a product with the sum's rounded
+// The exponent is (z - max) log2(e) / temperature, with the factor rounded once, the quotient a product with the sum's rounded
 // reciprocal: 2^-24 of x more for an exponent x, half a step more for a quotient, than two divisions for each column.
-template <int NT, int K>
+// kUnits: logits are taken in units of 2^-24, for temperatures above 2^100, where a difference that float32 does not hold
+// may be an exponent that it does.
+template <int NT, int K, bool kUnits = false>
 __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, float c, float* p) {
   __shared__ float red[NT / 64];
   const float* src = z + (size_t)blockIdx.x * n;
   float* dst = p + (size_t)blockIdx.x * n;
   float m = -INFINITY, s = 0.f;
   bool nan = false;
+  auto at = [&](int i) { return kUnits ? src[i] * kProbsUnit : src[i]; };
   if constexpr (K > 0) {
     float v[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = src[min(k * NT + (int)threadIdx.x, n - 1)];
+    for (int k = 0; k < K; ++k) v[k] = at(min(k * NT + (int)threadIdx.x, n - 1));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       nan |= v[k] != v[k];
@@ -77,7 +82,7 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
     for (int i0 = 0; i0 < n; i0 += kBatch * NT) {
       float v[kBatch], top = mine;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) v[k] = src[min(i0 + k * NT + (int)threadIdx.x, n - 1)];
+      for (int k = 0; k < kBatch; ++k) v[k] = at(min(i0 + k * NT + (int)threadIdx.x, n - 1));
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         nan |= v[k] != v[k];
@@ -97,7 +102,7 @@ __global__ __launch_bounds__(NT) void token_probs_kernel(const float* z, int n, 
     for (int i0 = begin; i0 < end; i0 += kBatch * NT) {
       float v[kBatch];
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) v[k] = src[min(i0 + k * NT + (int)threadIdx.x, end - 1)];
+      for (int k = 0; k < kBatch; ++k) v[k] = at(min(i0 + k * NT + (int)threadIdx.x, end - 1));
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const int i = i0 + k * NT + (int)threadIdx.x;

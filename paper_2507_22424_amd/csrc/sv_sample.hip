@@ -13,7 +13,10 @@ static int token_probs(const float* logits, int n_rows, int n_vocab, float tempe
   // Threads and columns a thread keeps, by the length of a row (us, 60 and 2000 or 960 rows: 256 columns 64 x 4 2.4, 3.0, 256 x 8
   // 2.6, 4.3; 2000 columns 256 x 8 2.8, 6.7, 1024 x 8 3.4, 13.8; 8000 columns 1024 x 8 3.7, 12.2, 1024 x 32 5.9, 22.7;
   // 32000 columns 1024 x 32 6.8, 42.7, two reads 9.0, 52.2).
-  if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, c, probs);
+  // (Below 2^100 a difference past the range of float32 is an exponent whose power is zero.)
+  if (temperature > 0x1p100f)
+    token_probs_kernel<1024, 0, true><<<n_rows, 1024, 0, st>>>(logits, n_vocab, (float)(1.4426950408889634 / ((double)temperature * kProbsUnit)), probs);
+  else if (n_vocab <= 256) token_probs_kernel<64, 4><<<n_rows, 64, 0, st>>>(logits, n_vocab, c, probs);
   else if (n_vocab <= 2048) token_probs_kernel<256, 8><<<n_rows, 256, 0, st>>>(logits, n_vocab, c, probs);
   else if (n_vocab <= 8192) token_probs_kernel<1024, 8><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);
   else if (n_vocab <= 32768) token_probs_kernel<1024, 32><<<n_rows, 1024, 0, st>>>(logits, n_vocab, c, probs);

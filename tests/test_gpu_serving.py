@@ -810,6 +810,25 @@ def test_token_probs_where_the_kernel_changes(rows, n):
     test_token_probs(rows, n)
 
 
+@pytest.mark.parametrize("n", [5, 300, 3000, 20000, 40000])
+def test_token_probs_at_the_ends_of_the_range(n):
+    """Temperatures from the smallest to the largest, logits whose differences float32 does not hold."""
+    gen = torch.Generator().manual_seed(n)
+    for t in (5e-39, 2e-38, 1e-30, 0.999, 1.0, 1.001, 1e30, 1e37, 1e38, 3e38):
+        z = (torch.randn(6, n, generator=gen) * max(t, 1.0)).clamp(-3.4e38, 3.4e38)
+        z[0] = -float("inf")
+        z[1, 1:] = -float("inf")
+        z[2, ::2] = torch.finfo(torch.float32).min
+        z[3], z[3, ::3] = 3.4e38, -3.4e38
+        z[4] *= 1e-30
+        d = z.cuda()
+        p = torch.empty_like(d)
+        sv.sv_token_probs(d, t, p)
+        _check_probs(f64(p.cpu()), f64(z), float(np.float32(t)))
+        sv.sv_token_probs(d, t, d)
+        assert torch.equal(d, p)
+
+
 @pytest.mark.parametrize("drawn", [True, False])
 @pytest.mark.parametrize("V", [40, 300, 5000, 20000, 40000])
 def test_rows_off_the_walk_have_no_effect(V, drawn):

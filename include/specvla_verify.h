@@ -430,7 +430,7 @@ int sv_paged_workspace_bytes(const sv_paged_cache *cache, int n_q_heads, int max
  * cores as sums of three bf16 numbers (2^-24 of each value).  Results are the same in every run.
  * SV_ERR_DTYPE for other cache types; SV_ERR_SHAPE if a size or alignment is outside the rules
  * above, n_q_heads is no multiple of n_kv_heads, n_seqs or n_q_heads exceeds 2^15, max_pages *
- * page_size 2^30, n_seqs * n_q_heads * ceil(max_len / 4096) 2^23, or scale is not finite; SV_ERR_WORKSPACE if the scratch is too small or misaligned. */
+ * page_size 2^30, n_seqs * n_q_heads * ceil(max_len / 4096) 2^23, or scale (or scale * log2(e)) is not finite; SV_ERR_WORKSPACE if the scratch is too small or misaligned. */
 int sv_paged_attention(const sv_paged_cache *cache, const int32_t *seq_len, int max_len,
                        const float *q, int n_q_heads, float scale, int window, int n_sink,
                        float *out, float *lse, int32_t *status, void *workspace, size_t ws_bytes,

@@ -139,14 +139,15 @@ int sv_paged_attention(const sv_paged_cache* cache, const int32_t* seq_len, int 
   const int rc = sv_paged_workspace_bytes(cache, n_q_heads, max_len, &need);
   if (rc != SV_OK) return rc;
   if (!seq_len || !q || !out || !workspace) return SV_ERR_NULL;
-  if (window < 0 || n_sink < 0 || !std::isfinite(scale) || (uintptr_t)q % 16 || (uintptr_t)out % 16) return SV_ERR_SHAPE;
+  const float scale2 = scale * 1.4426950408889634f;
+  if (window < 0 || n_sink < 0 || !std::isfinite(scale2) || (uintptr_t)q % 16 || (uintptr_t)out % 16) return SV_ERR_SHAPE;
   if ((uintptr_t)workspace % kAlign || ws_bytes < need) return SV_ERR_WORKSPACE;
   const int units = most_units(max_len, window, n_sink);
   const PagedPlan p = plan_paged(*cache, n_q_heads, units);
   PagedAttnArgs a;
   a.c = view(*cache); a.seq_len = seq_len; a.max_len = max_len; a.n_q = n_q_heads; a.window = window; a.n_sink = n_sink;
   a.n_blocks = p.n_blocks; a.n_split = p.n_split; a.split_units = p.split_units;
-  a.scale = scale * 1.4426950408889634f; a.q = q; a.out = out; a.lse = lse; a.status = status;
+  a.scale = scale2; a.q = q; a.out = out; a.lse = lse; a.status = status;
   a.part = (float*)((char*)workspace + p.part); a.part_ml = (float*)((char*)workspace + p.part_ml);
   hipStream_t st = (hipStream_t)stream;
   const unsigned groups = (unsigned)(((size_t)cache->n_seqs * cache->n_kv_heads * p.n_split + 7) / 8 * 8 * p.n_blocks);

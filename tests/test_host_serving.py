@@ -165,3 +165,11 @@ def test_sizes_past_32_bits_are_refused():
     tree, f, i, m = sv.Tree(4096, 4096, 4096, 1, 1), torch.zeros(1).expand(big + 1), ids.expand(big + 1), ws[:1].expand(big + 1)
     with pytest.raises(ValueError, match="sizes"):
         sv.sv_sampled_accept(tree, i, f[:, None], None, 0, f, f, big + 1, 0, m, i, i, i, i, i)
+
+
+def test_scales_that_float32_does_not_hold_in_base_two_are_refused():
+    """3e38 log2(e) is infinite: queries of zeros would become NaN."""
+    for scale in (3e38, -3e38, 2.4e38):
+        assert _attend(scale=scale) == -2
+    for scale in (2.3e38, -2.3e38):
+        assert _attend(scale=scale, ws_bytes=0) == -5        # past the check of the scale
